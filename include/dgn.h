@@ -440,6 +440,122 @@ int dgn_calibrate(void *buffer, size_t bytes, dgn_machine_rates *out, dgn_stream
  * well) or a negative DGN_ERR_*.  Synchronises `stream`; not thread safe (static host arrays). */
 int dgn_selftest_wave_ops(void *buffer, size_t bytes, dgn_stream stream);
 
+/* ---- values of tensors: what a pruned training step runs next ------------------------------------- */
+
+/* Element types.  Whatever the type, arithmetic is in 32 bits or more and a result is rounded once, when it is
+ * stored (to nearest, ties to even). */
+enum { DGN_F32 = 0, DGN_F16 = 1, DGN_BF16 = 2 };
+
+/* Gated linear recurrence: the operator that stands for an unrolled loop whose steps are linear in the state.
+ * Per sequence and channel, with h_{-1} = h0 (zero without one):
+ *      h_t = a_t h_{t-1} + u_t,    y_t = h_t
+ *      DGN_GATE_DECAY:    a_t = gate_t                 u_t = x_t
+ *      DGN_GATE_SIGMOID:  a_t = 1 / (1 + exp(-gate_t)) u_t = (1 - a_t) x_t
+ * The state is held in 32 bits.  Sequences are rows of one [num_tokens] list one after the other: sequence q has the
+ * rows seq_rowptr[q] .. seq_rowptr[q+1] - 1 (DEVICE int64 [num_seqs+1], ascending, within 0..num_tokens; any may be
+ * empty).  Rows before the first and after the last sequence are neither read nor written, so buffers may have room
+ * for more tokens than a batch has.  The lengths are never asked for on the host.  Row pointers that do not ascend
+ * give unspecified values; rows outside 0..num_tokens are not touched.
+ * A state that is no finite number stays none in its own sequence and channel and reaches no other. */
+enum { DGN_GATE_DECAY = 0, DGN_GATE_SIGMOID = 1 };
+
+typedef struct dgn_scan_desc {
+    int64_t num_tokens, num_seqs, num_channels;
+    int64_t gate_group;      /* consecutive channels that share a gate: divides num_channels; 1 = each its own */
+    int32_t dtype;           /* of x, gate, y and their gradients: DGN_F32 / DGN_F16 / DGN_BF16          */
+    int32_t gate_kind;       /* DGN_GATE_DECAY or DGN_GATE_SIGMOID                                        */
+    /* elements from one row to the next, at least the row's width; 0 = rows without gaps.  dx and dgate must not
+     * have rows that overlap anything else */
+    int64_t x_stride, gate_stride, y_stride, dy_stride, dx_stride, dgate_stride;
+} dgn_scan_desc;
+
+/* Bytes of scratch for dgn_scan_forward / dgn_scan_backward (the larger), and of the states that a forward pass
+ * keeps for the backward pass.  Either pointer may be NULL. */
+int dgn_scan_workspace(const dgn_scan_desc *desc, size_t *scratch_bytes, size_t *carry_bytes);
+
+/* x [num_tokens][num_channels], gate [num_tokens][num_channels / gate_group], h0 float [num_seqs][num_channels] or
+ * NULL -> y [num_tokens][num_channels], final float [num_seqs][num_channels] or NULL (the state after the last token;
+ * h0 of an empty sequence), carry: carry_bytes for dgn_scan_backward, or NULL.  All DEVICE, aligned to their
+ * elements; scratch to 8 bytes.  y may not overlap x or gate. */
+int dgn_scan_forward(const dgn_scan_desc *desc, const void *x, const void *gate, const int64_t *seq_rowptr,
+                     const float *h0, void *y, float *final, void *carry, void *scratch, size_t scratch_bytes,
+                     dgn_stream stream);
+
+/* Gradients for dy [num_tokens][num_channels] and dfinal float [num_seqs][num_channels] (or NULL: zero): dx, dgate (a
+ * shared gate's is the sum over its channels) and dh0 float (or NULL: not asked for).  x, gate, seq_rowptr and h0 as
+ * dgn_scan_forward had them, carry as it left it.  The states are computed again from there in 32 bits, so y is not
+ * needed.  The same inputs give the same bits. */
+int dgn_scan_backward(const dgn_scan_desc *desc, const void *x, const void *gate, const int64_t *seq_rowptr,
+                      const float *h0, const void *carry, const void *dy, const float *dfinal, void *dx, void *dgate,
+                      float *dh0, void *scratch, size_t scratch_bytes, dgn_stream stream);
+
+/* One token for each of desc->num_tokens rows (num_seqs is not looked at): row r's state is row slots[r] of state_in
+ * [num_slots][num_channels] (float) and goes to the same row of state_out, which may be state_in.  slots: DEVICE int32,
+ * or NULL: row r has slot r.  A row whose slot is outside 0..num_slots-1 (-1: an idle row of the batch) touches no
+ * state and gets y = 0.  No two rows may have the same slot. */
+int dgn_scan_step(const dgn_scan_desc *desc, int64_t num_slots, const void *x, const void *gate, const int32_t *slots,
+                  const float *state_in, float *state_out, void *y, dgn_stream stream);
+
+/* A list of tensors (the gradients of a step, its parameters ...): their addresses and sizes in device memory, so that
+ * one launch handles all.  Immutable; the tensors themselves are BORROWED: they must stay where they are for the life
+ * of the handle, their values may change. */
+typedef struct dgn_list dgn_list;
+typedef struct dgn_list_desc {
+    int64_t count;
+    void *const *data;       /* HOST [count]: DEVICE addresses, aligned to the element type */
+    const int64_t *numel;    /* HOST [count], 0 and up                                      */
+    const int32_t *dtype;    /* HOST [count]                                                */
+} dgn_list_desc;
+int dgn_list_workspace(const dgn_list_desc *desc, size_t *list_bytes);
+/* list_mem: DEVICE, 8-byte aligned, lives as long as the handle.  Synchronises the stream. */
+int dgn_list_build(const dgn_list_desc *desc, void *list_mem, size_t list_bytes, dgn_stream stream, dgn_list **out);
+void dgn_list_destroy(dgn_list *list);
+
+/* Which of up to 64 target sets need which tensor of a list: bit q of a word, as dgn_prune and dgn_backward_prune leave
+ * them in tensor_mask.  Entry i of a list has the word tensor_mask[tensor_ids[i]] (an id outside 0..num_words-1: no set
+ * needs it), without tensor_ids word i.  Without tensor_mask, or with a NULL dgn_reach (then there is one set), every set
+ * needs every tensor. */
+typedef struct dgn_reach {
+    int32_t num_sets;                /* 1..64 */
+    const uint64_t *tensor_mask;     /* DEVICE [num_words] or NULL */
+    int64_t num_words;
+    const int32_t *tensor_ids;       /* DEVICE [count] or NULL */
+} dgn_reach;
+
+/* norms[q] (DEVICE float [num_sets]) = square root of the sum of the squares of all elements of the tensors that set q
+ * needs; 0 where it needs none.  One pass over the tensors for all sets, sums in 64 bits in a fixed order: the same values
+ * give the same bits.  Tensors that no set needs do not count, whatever they hold. */
+int dgn_list_norms_workspace(const dgn_list *list, size_t *scratch_bytes);
+int dgn_list_norms(const dgn_list *list, const dgn_reach *reach, float *norms, void *scratch, size_t scratch_bytes,
+                   dgn_stream stream);
+
+/* out_i = f_i g_i, f_i the least of min(1, max_norm / (norms[q] + eps)) over the sets q that need tensor i, so that
+ * afterwards no set's norm is above max_norm; 1 where none does.  A norm that is infinite gives 0, one that is NaN gives
+ * NaN.  `out` has the sizes of `list` and may be `list` itself, or share single tensors with it. */
+int dgn_list_clip(const dgn_list *list, const dgn_list *out, const dgn_reach *reach, const float *norms, float max_norm,
+                  float eps, dgn_stream stream);
+
+/* Adam with decoupled weight decay, the updater's step of the paper's Sec. 3.2 as one operator: with g = f_i times the
+ * gradient (f_i as in dgn_list_clip if norms are given, else 1)
+ *      m' = beta1 m + (1 - beta1) g,   v' = beta2 v + (1 - beta2) g^2
+ *      p' = p - lr (m' / (1 - beta1^step) / (sqrt(v' / (1 - beta2^step)) + eps) + weight_decay p)
+ * Parameters and moments are DGN_F32, gradients of any type; out_* may be the inputs themselves or other tensors (an update
+ * graph without cycles).  copy (or NULL): p' once more, rounded to that list's types.  A tensor that no set needs, and with
+ * skip_nonfinite one of which a set's norm is no finite number, keeps its p, m and v. */
+typedef struct dgn_adam_lists {
+    const dgn_list *grad, *param, *m, *v;
+    const dgn_list *out_param, *out_m, *out_v;   /* NULL: in place */
+    const dgn_list *copy;                        /* or NULL        */
+} dgn_adam_lists;
+typedef struct dgn_adam_options {
+    double lr, beta1, beta2, eps, weight_decay;
+    int64_t step;                    /* of this update: 1 for the first */
+    int32_t skip_nonfinite;
+    float max_norm, clip_eps;        /* used with norms */
+} dgn_adam_options;
+int dgn_list_adam(const dgn_adam_lists *lists, const dgn_reach *reach, const float *norms,
+                  const dgn_adam_options *options, dgn_stream stream);
+
 /* ---- misc ---------------------------------------------------------------------------------- */
 const char *dgn_strerror(int code);
 int dgn_version(void);

@@ -8,3 +8,4 @@ from .binding import *  # noqa: F401,F403
 from .binding import (DeviceGraph, PruneBuffers, BackwardPruneBuffers, InplaceBuffers, ReadoutBuffers, TransactionCache,
                       DgnError, EXPORTS,
                       LIB_PATH)  # noqa: F401
+from .values import AdamBuffers, GradientBuffers, ScanBuffers, ScanStepBuffers, TensorList  # noqa: F401

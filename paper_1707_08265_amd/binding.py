@@ -27,12 +27,18 @@ DGN_ERR_NOT_TOPOLOGICAL = -7
 DGN_ERR_HIP = -8
 DGN_ERR_BAD_CSR = -9
 
+DGN_F32, DGN_F16, DGN_BF16 = 0, 1, 2
+DGN_GATE_DECAY, DGN_GATE_SIGMOID = 0, 1
+
 EXPORTS = [
     "dgn_graph_build_workspace", "dgn_graph_build", "dgn_graph_from_csr_workspace", "dgn_graph_from_csr",
     "dgn_graph_get_csr", "dgn_graph_get_sizes", "dgn_graph_destroy", "dgn_prune_workspace", "dgn_prune",
     "dgn_prune_words", "dgn_keep_compact", "dgn_keep_compact_static_limits", "dgn_keep_compact_static", "dgn_backward_prune_workspace", "dgn_backward_prune", "dgn_inplace_workspace",
     "dgn_inplace", "dgn_inplace_kept", "dgn_ignore_mask", "dgn_per_set_lists_workspace", "dgn_per_set_lists",
     "dgn_target_digest_workspace", "dgn_target_digest", "dgn_calibrate", "dgn_selftest_wave_ops", "dgn_strerror",
+    "dgn_scan_workspace", "dgn_scan_forward", "dgn_scan_backward", "dgn_scan_step",
+    "dgn_list_workspace", "dgn_list_build", "dgn_list_destroy", "dgn_list_norms_workspace", "dgn_list_norms",
+    "dgn_list_clip", "dgn_list_adam",
     "dgn_version",
     "dgn_last_hip_error",
 ]
@@ -74,6 +80,30 @@ class dgn_machine_rates(ctypes.Structure):
 
     def as_dict(self):
         return {n: round(float(getattr(self, n)), 3) for n, _ in self._fields_[:12]} | {"buffer_bytes": int(self.buffer_bytes)}
+
+
+class dgn_scan_desc(ctypes.Structure):
+    _fields_ = [("num_tokens", c_int64), ("num_seqs", c_int64), ("num_channels", c_int64), ("gate_group", c_int64),
+                ("dtype", c_int32), ("gate_kind", c_int32), ("x_stride", c_int64), ("gate_stride", c_int64),
+                ("y_stride", c_int64), ("dy_stride", c_int64), ("dx_stride", c_int64), ("dgate_stride", c_int64)]
+
+
+class dgn_list_desc(ctypes.Structure):
+    _fields_ = [("count", c_int64), ("data", c_void_p), ("numel", c_void_p), ("dtype", c_void_p)]
+
+
+class dgn_reach(ctypes.Structure):
+    _fields_ = [("num_sets", c_int32), ("tensor_mask", c_void_p), ("num_words", c_int64), ("tensor_ids", c_void_p)]
+
+
+class dgn_adam_lists(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in ("grad", "param", "m", "v", "out_param", "out_m", "out_v", "copy")]
+
+
+class dgn_adam_options(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("step", c_int64), ("skip_nonfinite", c_int32),
+                ("max_norm", ctypes.c_float), ("clip_eps", ctypes.c_float)]
 
 
 PHASES = ["clear", "seed", "traverse", "count", "scan", "scatter", "total"]
@@ -124,6 +154,18 @@ def _load() -> ctypes.CDLL:
                                       c_size_t, c_void_p]
     lib.dgn_calibrate.argtypes = [c_void_p, c_size_t, POINTER(dgn_machine_rates), c_void_p]
     lib.dgn_selftest_wave_ops.argtypes = [c_void_p, c_size_t, c_void_p]
+    lib.dgn_scan_workspace.argtypes = [POINTER(dgn_scan_desc), POINTER(c_size_t), POINTER(c_size_t)]
+    lib.dgn_scan_forward.argtypes = [POINTER(dgn_scan_desc)] + [c_void_p] * 8 + [c_size_t, c_void_p]
+    lib.dgn_scan_backward.argtypes = [POINTER(dgn_scan_desc)] + [c_void_p] * 11 + [c_size_t, c_void_p]
+    lib.dgn_scan_step.argtypes = [POINTER(dgn_scan_desc), c_int64] + [c_void_p] * 7
+    lib.dgn_list_workspace.argtypes = [POINTER(dgn_list_desc), POINTER(c_size_t)]
+    lib.dgn_list_build.argtypes = [POINTER(dgn_list_desc), c_void_p, c_size_t, c_void_p, POINTER(c_void_p)]
+    lib.dgn_list_destroy.argtypes = [c_void_p]
+    lib.dgn_list_destroy.restype = None
+    lib.dgn_list_norms_workspace.argtypes = [c_void_p, POINTER(c_size_t)]
+    lib.dgn_list_norms.argtypes = [c_void_p, POINTER(dgn_reach), c_void_p, c_void_p, c_size_t, c_void_p]
+    lib.dgn_list_clip.argtypes = [c_void_p, c_void_p, POINTER(dgn_reach), c_void_p, ctypes.c_float, ctypes.c_float, c_void_p]
+    lib.dgn_list_adam.argtypes = [POINTER(dgn_adam_lists), POINTER(dgn_reach), c_void_p, POINTER(dgn_adam_options), c_void_p]
     lib.dgn_inplace_workspace.argtypes = [c_void_p, POINTER(c_size_t)]
     lib.dgn_inplace.argtypes = [c_void_p, c_void_p, ctypes.c_uint64, c_void_p, c_void_p, c_void_p, c_size_t,
                                 POINTER(c_int32), c_void_p]
@@ -379,6 +421,68 @@ def dgn_inplace_kept(handle, op_mask, select, kept_ops, kept_count, rename, rena
                                _dp(rename), _dp(renamed_count), _dp(scratch), scratch_bytes, ctypes.byref(rounds),
                                _stream(stream))
     return rc, rounds.value
+
+
+def _ref(struct):
+    return ctypes.byref(struct) if struct is not None else None
+
+
+def dgn_scan_workspace(desc):
+    """Returns (rc, scratch bytes, bytes of the states kept for the backward pass)."""
+    s, c = c_size_t(0), c_size_t(0)
+    rc = _lib.dgn_scan_workspace(_ref(desc), ctypes.byref(s), ctypes.byref(c))
+    return rc, s.value, c.value
+
+
+def dgn_scan_forward(desc, x, gate, seq_rowptr, h0, y, final, carry, scratch, scratch_bytes, stream=None) -> int:
+    return _lib.dgn_scan_forward(_ref(desc), _dp(x), _dp(gate), _dp(seq_rowptr), _dp(h0), _dp(y), _dp(final), _dp(carry),
+                                 _dp(scratch), scratch_bytes, _stream(stream))
+
+
+def dgn_scan_backward(desc, x, gate, seq_rowptr, h0, carry, dy, dfinal, dx, dgate, dh0, scratch, scratch_bytes,
+                      stream=None) -> int:
+    return _lib.dgn_scan_backward(_ref(desc), _dp(x), _dp(gate), _dp(seq_rowptr), _dp(h0), _dp(carry), _dp(dy), _dp(dfinal),
+                                  _dp(dx), _dp(dgate), _dp(dh0), _dp(scratch), scratch_bytes, _stream(stream))
+
+
+def dgn_scan_step(desc, num_slots, x, gate, slots, state_in, state_out, y, stream=None) -> int:
+    return _lib.dgn_scan_step(_ref(desc), num_slots, _dp(x), _dp(gate), _dp(slots), _dp(state_in), _dp(state_out), _dp(y),
+                              _stream(stream))
+
+
+def dgn_list_workspace(desc):
+    n = c_size_t(0)
+    rc = _lib.dgn_list_workspace(_ref(desc), ctypes.byref(n))
+    return rc, n.value
+
+
+def dgn_list_build(desc, list_mem, list_bytes, stream=None):
+    """Returns (rc, handle)."""
+    h = c_void_p(None)
+    rc = _lib.dgn_list_build(_ref(desc), _dp(list_mem), list_bytes, _stream(stream), ctypes.byref(h))
+    return rc, h.value
+
+
+def dgn_list_destroy(handle):
+    _lib.dgn_list_destroy(handle)
+
+
+def dgn_list_norms_workspace(handle):
+    n = c_size_t(0)
+    rc = _lib.dgn_list_norms_workspace(handle, ctypes.byref(n))
+    return rc, n.value
+
+
+def dgn_list_norms(handle, reach, norms, scratch, scratch_bytes, stream=None) -> int:
+    return _lib.dgn_list_norms(handle, _ref(reach), _dp(norms), _dp(scratch), scratch_bytes, _stream(stream))
+
+
+def dgn_list_clip(handle, out, reach, norms, max_norm, eps=1e-6, stream=None) -> int:
+    return _lib.dgn_list_clip(handle, out, _ref(reach), _dp(norms), max_norm, eps, _stream(stream))
+
+
+def dgn_list_adam(lists, reach, norms, options, stream=None) -> int:
+    return _lib.dgn_list_adam(_ref(lists), _ref(reach), _dp(norms), _ref(options), _stream(stream))
 
 
 # ------------------------------------------------------------------------------------------------

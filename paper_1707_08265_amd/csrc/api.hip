@@ -646,6 +646,8 @@ int build_from_lists(dgn_graph *h, const dgn_coo_desc *d, const GraphLayout &L, 
 
 }  // namespace
 
+namespace dgn { int note_hip_error(hipError_t e) { return hip_fail(e); } }
+
 extern "C" {
 
 int dgn_version(void) { return DGN_VERSION; }

@@ -282,6 +282,8 @@ template <bool stream> __device__ __forceinline__ void store16(void *p, int a, i
     else *reinterpret_cast<Int4Vec *>(p) = v;
 }
 
+int note_hip_error(hipError_t e);   // what dgn_last_hip_error() reports on this thread; returns DGN_ERR_HIP
+
 // ---- launch wrappers (each returns a hipError_t; nothing synchronises) -------------------------
 struct FillRegion { void *ptr; size_t bytes; };   // ptr 8-byte aligned, bytes multiple of 8
 hipError_t launch_clear(const FillRegion *regions, int num_regions, hipStream_t s);

@@ -1,0 +1,212 @@
+"""Owners of buffers for the operators on tensor values: the gated linear recurrence, and lists of tensors with their
+norms, clipping and update.  Allocation, checks of types and shapes, and marshalling only.
+
+The library sees addresses; what a tensor's type, shape and strides say is checked here.  Every method raises
+``DgnError`` for what is refused, by these checks or by the library.  Kernels run on the current stream, or on
+``stream``; a caller who uses another stream than the one its tensors belong to orders the two, as for any kernel.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import numpy as np
+import torch
+
+from . import binding as b
+
+DTYPES = {torch.float32: b.DGN_F32, torch.float16: b.DGN_F16, torch.bfloat16: b.DGN_BF16}
+GATES = {"decay": b.DGN_GATE_DECAY, "sigmoid": b.DGN_GATE_SIGMOID}
+
+
+def _need(ok, where):
+    if not ok:
+        raise b.DgnError(b.DGN_ERR_INVALID_ARG, where)
+
+
+def _rows(t, rows, width, dtype, device, where):
+    """Address and row stride of a matrix whose rows have no gaps inside."""
+    _need(isinstance(t, torch.Tensor) and t.dtype is dtype and t.device == device and t.dim() == 2
+          and t.shape[0] == rows and t.shape[1] == width and (t.stride(1) == 1 or width <= 1)
+          and (t.stride(0) >= width or rows <= 1), where)
+    return t.data_ptr(), t.stride(0) if rows > 1 else 0
+
+
+def _dense(t, shape, dtype, device, where):
+    if t is None:
+        return None
+    _need(isinstance(t, torch.Tensor) and t.dtype is dtype and t.device == device and tuple(t.shape) == shape
+          and t.is_contiguous(), where)
+    return t.data_ptr()
+
+
+def _desc(tokens, seqs, channels, group, kind, dtype):
+    _need(kind in GATES and dtype in DTYPES, "gate kind or element type")
+    return b.dgn_scan_desc(num_tokens=tokens, num_seqs=seqs, num_channels=channels, gate_group=group,
+                           dtype=DTYPES[dtype], gate_kind=GATES[kind])
+
+
+class ScanBuffers:
+    """Outputs and scratch of the gated linear recurrence over ``num_seqs`` sequences in ``num_tokens`` rows.
+
+    ``forward`` writes ``y`` and ``final``; with ``train`` it keeps the states that ``backward`` starts from, and
+    ``backward``, given the same inputs, writes ``dx``, ``dgate`` and ``dh0``.  ``gate_group`` channels share a gate."""
+
+    def __init__(self, num_tokens, num_seqs, num_channels, gate_group=1, kind="sigmoid", dtype=torch.bfloat16,
+                 train=False, device="cuda"):
+        self._d = _desc(num_tokens, num_seqs, num_channels, gate_group, kind, dtype)
+        rc, sb, cb = b.dgn_scan_workspace(self._d)
+        b._check(rc, "dgn_scan_workspace")
+        self.num_tokens, self.num_seqs, self.num_channels = num_tokens, num_seqs, num_channels
+        self.num_heads, self.dtype, self.train = num_channels // gate_group, dtype, bool(train)
+        # rows that belong to no sequence are not written: zero until they are
+        new = lambda *shape, dtype=dtype: torch.zeros(shape, dtype=dtype, device=device)  # noqa: E731
+        self.y = new(num_tokens, num_channels)
+        self.final = new(num_seqs, num_channels, dtype=torch.float32)
+        self.device = self.y.device
+        self._scratch, self._scratch_bytes = torch.empty(sb, dtype=torch.uint8, device=device), sb
+        self._carry = torch.empty(cb, dtype=torch.uint8, device=device) if train else None
+        if train:
+            self.dx, self.dgate = new(num_tokens, num_channels), new(num_tokens, self.num_heads)
+            self.dh0 = new(num_seqs, num_channels, dtype=torch.float32)
+
+    def _inputs(self, x, gate, seq_rowptr, h0):
+        d, dev = self._d, self.device
+        px, d.x_stride = _rows(x, self.num_tokens, self.num_channels, self.dtype, dev, "x")
+        pg, d.gate_stride = _rows(gate, self.num_tokens, self.num_heads, self.dtype, dev, "gate")
+        pr = _dense(seq_rowptr, (self.num_seqs + 1,), torch.int64, dev, "seq_rowptr")
+        return px, pg, pr, _dense(h0, (self.num_seqs, self.num_channels), torch.float32, dev, "h0")
+
+    def forward(self, x, gate, seq_rowptr, h0=None, stream=None):
+        """``x`` [tokens, channels], ``gate`` [tokens, heads], ``seq_rowptr`` int64 [seqs + 1], ``h0`` float [seqs, channels]."""
+        px, pg, pr, ph = self._inputs(x, gate, seq_rowptr, h0)
+        b._check(b._lib.dgn_scan_forward(ctypes.byref(self._d), px, pg, pr, ph, self.y.data_ptr(), self.final.data_ptr(),
+                                         b._dp(self._carry), self._scratch.data_ptr(), self._scratch_bytes,
+                                         b._stream(stream)), "dgn_scan_forward")
+
+    def backward(self, x, gate, seq_rowptr, dy, h0=None, dfinal=None, stream=None):
+        """Gradients for ``dy`` [tokens, channels] and ``dfinal`` float [seqs, channels] of the last ``forward``."""
+        _need(self.train, "backward of buffers made without train")
+        px, pg, pr, ph = self._inputs(x, gate, seq_rowptr, h0)
+        py, self._d.dy_stride = _rows(dy, self.num_tokens, self.num_channels, self.dtype, self.device, "dy")
+        pf = _dense(dfinal, (self.num_seqs, self.num_channels), torch.float32, self.device, "dfinal")
+        b._check(b._lib.dgn_scan_backward(ctypes.byref(self._d), px, pg, pr, ph, b._dp(self._carry), py, pf,
+                                          self.dx.data_ptr(), self.dgate.data_ptr(), self.dh0.data_ptr(),
+                                          self._scratch.data_ptr(), self._scratch_bytes, b._stream(stream)),
+                 "dgn_scan_backward")
+
+
+class ScanStepBuffers:
+    """Output of one token of the recurrence for each of ``num_rows`` rows, on states in a pool of ``num_slots``."""
+
+    def __init__(self, num_rows, num_slots, num_channels, gate_group=1, kind="sigmoid", dtype=torch.bfloat16, device="cuda"):
+        self._d = _desc(num_rows, 0, num_channels, gate_group, kind, dtype)
+        b._check(b.dgn_scan_workspace(self._d)[0], "dgn_scan_workspace")
+        self.num_rows, self.num_slots, self.num_channels = num_rows, num_slots, num_channels
+        self.num_heads, self.dtype = num_channels // gate_group, dtype
+        self.y = torch.empty(num_rows, num_channels, dtype=dtype, device=device)
+        self.device = self.y.device
+
+    def step(self, x, gate, slots, state_in, state_out=None, stream=None):
+        """Row r takes its state from row ``slots[r]`` of ``state_in`` (float [slots, channels]) and leaves it in the same
+        row of ``state_out`` (default: ``state_in`` itself).  ``slots``: int32, -1 for an idle row, or None: row r."""
+        d, dev, pool = self._d, self.device, (self.num_slots, self.num_channels)
+        px, d.x_stride = _rows(x, self.num_rows, self.num_channels, self.dtype, dev, "x")
+        pg, d.gate_stride = _rows(gate, self.num_rows, self.num_heads, self.dtype, dev, "gate")
+        ps = _dense(slots, (self.num_rows,), torch.int32, dev, "slots")
+        pi = _dense(state_in, pool, torch.float32, dev, "state_in")
+        po = pi if state_out is None else _dense(state_out, pool, torch.float32, dev, "state_out")
+        b._check(b._lib.dgn_scan_step(ctypes.byref(d), self.num_slots, px, pg, ps, pi, po, self.y.data_ptr(), b._stream(stream)),
+                 "dgn_scan_step")
+
+
+class TensorList:
+    """A list of contiguous tensors of one device whose addresses the library holds; keeps the tensors alive."""
+
+    def __init__(self, tensors, stream=None):
+        self.tensors = list(tensors)
+        n = len(self.tensors)
+        dev = self.tensors[0].device if n else torch.device("cuda", torch.cuda.current_device())
+        for t in self.tensors:
+            _need(isinstance(t, torch.Tensor) and t.dtype in DTYPES and t.device == dev and t.is_contiguous(), "TensorList")
+        self.device = dev
+        self._numel = np.array([t.numel() for t in self.tensors] or [0], dtype=np.int64)
+        data = np.array([t.data_ptr() for t in self.tensors] or [0], dtype=np.uint64)
+        types = np.array([DTYPES[t.dtype] for t in self.tensors] or [0], dtype=np.int32)
+        desc = b.dgn_list_desc(count=n, data=data.ctypes.data, numel=self._numel.ctypes.data, dtype=types.ctypes.data)
+        self.handle = None
+        rc, nb = b.dgn_list_workspace(desc)
+        b._check(rc, "dgn_list_workspace")
+        self._mem = torch.empty(nb, dtype=torch.uint8, device=dev)
+        rc, self.handle = b.dgn_list_build(desc, self._mem, nb, stream)
+        b._check(rc, "dgn_list_build")
+
+    def __len__(self):
+        return len(self.tensors)
+
+    def close(self):
+        if self.handle:
+            b.dgn_list_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        if getattr(self, "handle", None):
+            self.close()
+
+
+def _reach(lst, num_sets, mask, ids):
+    _need(ids is None or mask is not None, "tensor_ids without tensor_mask")
+    if mask is None:
+        return b.dgn_reach(num_sets, None, 0, None)
+    _need(mask.dtype is torch.int64 and mask.dim() == 1 and mask.is_contiguous() and mask.device == lst.device, "tensor_mask")
+    return b.dgn_reach(num_sets, mask.data_ptr(), mask.numel(), _dense(ids, (len(lst),), torch.int32, lst.device, "tensor_ids"))
+
+
+class GradientBuffers:
+    """Norms of a list of gradients for up to 64 target sets, and clipping by them.
+
+    ``mask``: int64 words as ``PruneBuffers.prune`` or ``backward_prune`` leave them in ``tensor_mask`` (bit q: target set
+    q needs the tensor); ``ids``: int32, the graph's tensor that each entry of the list stands for.  Without ``mask``
+    every set needs every tensor."""
+
+    def __init__(self, grads: TensorList, num_sets: int = 1):
+        self.grads, self.num_sets = grads, num_sets
+        rc, sb = b.dgn_list_norms_workspace(grads.handle)
+        b._check(rc, "dgn_list_norms_workspace")
+        self.norms = torch.empty(max(num_sets, 1), dtype=torch.float32, device=grads.device)
+        self._scratch, self._scratch_bytes = torch.empty(sb, dtype=torch.uint8, device=grads.device), sb
+
+    def norm(self, mask=None, ids=None, stream=None):
+        """Fills ``norms`` [num_sets]."""
+        r = _reach(self.grads, self.num_sets, mask, ids)
+        b._check(b._lib.dgn_list_norms(self.grads.handle, ctypes.byref(r), self.norms.data_ptr(), self._scratch.data_ptr(),
+                                       self._scratch_bytes, b._stream(stream)), "dgn_list_norms")
+
+    def clip(self, out: TensorList, max_norm, eps=1e-6, mask=None, ids=None, stream=None):
+        """Writes the gradients, scaled so that no set's norm is above ``max_norm``, to ``out`` (may be the list itself);
+        goes by ``norms`` as the last ``norm`` call left them."""
+        r = _reach(self.grads, self.num_sets, mask, ids)
+        b._check(b._lib.dgn_list_clip(self.grads.handle, out.handle, ctypes.byref(r), self.norms.data_ptr(), max_norm, eps,
+                                      b._stream(stream)), "dgn_list_clip")
+
+
+class AdamBuffers:
+    """The lists of an Adam update: gradients, parameters and both moments (float32), where the new ones go (default: in
+    place), and a list that receives the new parameters once more in its own types."""
+
+    def __init__(self, grads: TensorList, params: TensorList, m: TensorList, v: TensorList, out_params=None, out_m=None,
+                 out_v=None, copy=None):
+        self._all = (grads, params, m, v, out_params, out_m, out_v, copy)
+        self.grads = grads
+        self._lists = b.dgn_adam_lists(*(None if t is None else t.handle for t in self._all))
+
+    def step(self, lr, beta1, beta2, eps, weight_decay, step, norms=None, max_norm=1.0, clip_eps=1e-6, mask=None, ids=None,
+             num_sets=None, skip_nonfinite=False, stream=None):
+        """``norms`` (of ``GradientBuffers``): gradients are scaled as ``clip`` would; ``num_sets`` defaults to their number."""
+        if norms is not None:
+            num_sets = norms.numel() if num_sets is None else num_sets
+            _need(norms.dtype is torch.float32 and norms.is_contiguous() and norms.numel() >= num_sets
+                  and norms.device == self.grads.device, "norms")
+        r = _reach(self.grads, (64 if mask is not None else 1) if num_sets is None else num_sets, mask, ids)
+        o = b.dgn_adam_options(lr, beta1, beta2, eps, weight_decay, step, int(skip_nonfinite), max_norm, clip_eps)
+        b._check(b._lib.dgn_list_adam(ctypes.byref(self._lists), ctypes.byref(r), None if norms is None else norms.data_ptr(),
+                                      ctypes.byref(o), b._stream(stream)), "dgn_list_adam")

@@ -1,0 +1,314 @@
+"""Norms, clipping and update over lists of tensors on the GPU against their plain forms in 64 bits."""
+import pytest
+import torch
+
+import values_oracle as vo
+
+pytestmark = pytest.mark.gpu
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+SIZES = [1, 0, 2, 3, 5, 8, 63, 257, 4099, 0, 16383, 16384, 16385, 40000, 1, 70001]
+ADAM = dict(lr=1e-2, beta1=0.9, beta2=0.95, eps=1e-8, weight_decay=0.1, step=3)
+
+
+@pytest.fixture(scope="module")
+def dgn():
+    assert torch.cuda.is_available(), "these tests need the GPU"
+    import paper_1707_08265_amd as d
+    return d
+
+
+def tensors(sizes=SIZES, types=TYPES, scale=0.02, seed=0, odd=True):
+    """One tensor for each size, types in turn, at addresses that are aligned to their elements alone where `odd`."""
+    gen = torch.Generator().manual_seed(seed)
+    out = []
+    for i, n in enumerate(sizes):
+        store = torch.empty(n + 16, dtype=types[i % len(types)], device="cuda")
+        at = (i * 3) % 8 if odd else 0
+        store[at:at + n] = (torch.randn(n, generator=gen) * scale).to(store.dtype).cuda()
+        out.append(store[at:at + n])
+    return out
+
+
+def words_of(n, sets, seed=1):
+    gen = torch.Generator().manual_seed(seed)
+    bits = (torch.rand(n, sets, generator=gen) < 0.3).long()
+    bits[n // 2] = 0                                     # a tensor that no set needs
+    bits[:, sets // 2] = 0                               # a set that needs no tensor
+    return (bits << torch.arange(sets)).sum(1)
+
+
+def signed(words):
+    return [w & (2**64 - 1) for w in words.tolist()]
+
+
+@pytest.mark.parametrize("sets", [1, 2, 5, 63, 64])
+def test_norms_of_sets(dgn, sets):
+    g = tensors()
+    words = words_of(len(g), sets) if sets > 1 else torch.ones(len(g), dtype=torch.int64)
+    print(f"norms: {sets} sets", flush=True)
+    b = dgn.GradientBuffers(dgn.TensorList(g), sets)
+    b.norm(words.cuda())
+    want = vo.norms(g, signed(words), sets)
+    # 64-bit sums: what is left is the square root's rounding to 32 bits
+    assert ((b.norms.double().cpu() - want).abs() <= 2.0**-23 * want).all()
+    first = b.norms.clone()
+    b.norm(words.cuda())
+    assert torch.equal(first, b.norms)
+    b.norm()                                             # without a mask every set needs every tensor
+    whole = vo.norms(g, [1] * len(g), 1)
+    assert ((b.norms.double().cpu() - whole).abs() <= 2.0**-23 * whole).all()
+
+
+def test_norms_by_tensor_ids_and_what_does_not_count(dgn):
+    g = tensors()
+    n, sets = len(g), 6
+    gen = torch.Generator().manual_seed(4)
+    mask = (torch.rand(1000, sets, generator=gen) < 0.4).long() @ (2 ** torch.arange(sets)) | (1 << 60)
+    ids = torch.randperm(1000, generator=gen)[:n].to(torch.int32)
+    ids[3], ids[4] = -1, 1000                            # no tensor of the graph: nobody needs them
+    words = [0 if i in (3, 4) else int(mask[ids[i]]) for i in range(n)]
+    words[8] = 0
+    mask[ids[8]] = 0
+    for i in (3, 4, 8):
+        g[i].fill_(float("nan"))
+    b = dgn.GradientBuffers(dgn.TensorList(g), sets)
+    b.norm(mask.cuda(), ids.cuda())
+    clean = [torch.zeros_like(t) if i in (3, 4, 8) else t for i, t in enumerate(g)]
+    want = vo.norms(clean, words, sets)
+    assert ((b.norms.double().cpu() - want).abs() <= 2.0**-23 * want).all()
+
+
+def test_norms_of_large_and_small_numbers(dgn):
+    """Squares that 32 bits do not hold."""
+    for scale in (1e25, 1e-30):
+        g = tensors([5000, 20000], [torch.float32, torch.bfloat16], scale)
+        b = dgn.GradientBuffers(dgn.TensorList(g))
+        b.norm()
+        want = vo.norms(g, [1, 1], 1)
+        assert float(want[0]) > 0 and abs(float(b.norms[0]) - float(want[0])) <= 2.0**-23 * float(want[0])
+    for bad in (float("nan"), float("inf")):
+        g = tensors()
+        g[13][777] = bad
+        words = torch.ones(len(g), dtype=torch.int64) * 3
+        words[13] = 2
+        b = dgn.GradientBuffers(dgn.TensorList(g), 2)
+        b.norm(words.cuda())
+        assert b.norms[0].isfinite() and (b.norms[1].isnan() if bad != bad else b.norms[1] == float("inf"))
+
+
+@pytest.mark.parametrize("sets", [1, 7, 64])
+@pytest.mark.parametrize("max_norm", [0.0, 0.05, 1.0, 1e6])
+def test_clip(dgn, sets, max_norm):
+    g = tensors()
+    words = words_of(len(g), sets) if sets > 1 else torch.ones(len(g), dtype=torch.int64)
+    before = [t.clone() for t in g]
+    out = tensors(seed=5)
+    for i in (2, 10, 13):
+        out[i] = g[i]                                    # some in place, some elsewhere
+    lst, to = dgn.TensorList(g), dgn.TensorList(out)
+    b = dgn.GradientBuffers(lst, sets)
+    b.norm(words.cuda())
+    b.clip(to, max_norm, mask=words.cuda())
+    f = vo.factors(b.norms, signed(words), max_norm, 1e-6)
+    for i, (t, o) in enumerate(zip(before, out)):
+        if f[i] == 1.0:
+            assert torch.equal(t, o), i                  # not rounded, not touched
+        else:
+            want = t.double().cpu() * f[i]
+            vo.within(o, want, 4 * vo.U32 * want.abs(), f"tensor {i}")
+        if i not in (2, 10, 13):
+            assert torch.equal(t, g[i]), i
+    if max_norm > 0:
+        c = dgn.GradientBuffers(to, sets)
+        c.norm(words.cuda())
+        assert (c.norms <= max_norm * (1 + 2.0**-7) + 1e-6).all()      # each element is rounded to its type, up to 2^-8
+
+
+def test_clip_by_norms_that_are_no_numbers(dgn):
+    g = tensors()
+    b = dgn.GradientBuffers(dgn.TensorList(g), 3)
+    b.norms.copy_(torch.tensor([float("inf"), float("nan"), 100.0]))
+    words = torch.tensor([(1, 2, 4, 0, 5, 6)[i % 6] for i in range(len(g))])
+    out = tensors(seed=2)
+    b.clip(dgn.TensorList(out), 1.0, mask=words.cuda())
+    for i, (t, o) in enumerate(zip(g, out)):
+        w = int(words[i])
+        if w & 2:
+            assert o.isnan().all()
+        elif w & 1:
+            assert (o == 0).all()
+        elif w == 0:
+            assert torch.equal(o, t)
+        else:
+            vo.within(o, t.double().cpu() / (100 + 1e-6), 4 * vo.U32 * t.double().cpu().abs(), "least")
+
+
+@pytest.mark.parametrize("how", ["in place", "elsewhere", "copy"])
+@pytest.mark.parametrize("types", [TYPES, [torch.bfloat16], [torch.float32]])
+def test_adam(dgn, how, types):
+    print(f"adam: {how}, {types}", flush=True)
+    f32 = [torch.float32]
+    g, p, m = tensors(types=types), tensors(types=f32, seed=1), tensors(types=f32, seed=2)
+    v = [t.square_() for t in tensors(types=f32, seed=3)]
+    old = [[t.clone() for t in ts] for ts in (p, m, v)]
+    lists = [dgn.TensorList(t) for t in (g, p, m, v)]
+    kw, outs = {}, (p, m, v)
+    if how != "in place":
+        outs = tuple(tensors(types=f32, seed=9 + k, odd=False) for k in range(3))
+        kw = dict(zip(("out_params", "out_m", "out_v"), map(dgn.TensorList, outs)))
+    copies = None
+    if how == "copy":
+        copies = tensors(types=TYPES, seed=4)
+        kw["copy"] = dgn.TensorList(copies)
+    b = dgn.GradientBuffers(lists[0], 5)
+    words = words_of(len(g), 5)
+    b.norm(words.cuda())
+    dgn.AdamBuffers(*lists, **kw).step(**ADAM, norms=b.norms, max_norm=0.5, mask=words.cuda())
+    f = vo.factors(b.norms, signed(words), 0.5, 1e-6)
+    for i in range(len(g)):
+        was = [o[i] for o in old]
+        if int(words[i]) == 0:
+            for o, w in zip(outs, was):
+                assert torch.equal(o[i], w), i
+            want = (was[0].double().cpu(), torch.zeros(SIZES[i], dtype=torch.float64))
+        else:
+            (want, *_), = [vo.adam(*was, g[i].double().cpu() * f[i], **ADAM)]
+            for o, (value, error), name in zip(outs, vo.adam(*was, g[i].double().cpu() * f[i], **ADAM), "pmv"):
+                vo.within(o[i], value, error, f"{name} of tensor {i}")
+        if copies is not None:
+            assert torch.equal(copies[i], outs[0][i].to(copies[i].dtype)), i
+        if how != "in place":
+            assert all(torch.equal(t[i], w) for t, w in zip((p, m, v), was))
+
+
+def test_adam_without_clipping_and_over_steps(dgn):
+    """No norms, no mask: every tensor, gradients as they are; five steps in place."""
+    f32 = [torch.float32]
+    g, p, m, v = (tensors([3000, 1, 20011], f32, seed=k) for k in range(4))
+    for t in (*m, *v):
+        t.zero_()
+    a = dgn.AdamBuffers(*(dgn.TensorList(t) for t in (g, p, m, v)))
+    for step in range(1, 6):
+        old = [[t.clone() for t in ts] for ts in (p, m, v)]
+        a.step(**{**ADAM, "step": step})
+        for i in range(3):
+            for o, (value, error) in zip((p, m, v), vo.adam(*(t[i] for t in old), g[i], **{**ADAM, "step": step})):
+                vo.within(o[i], value, error, f"step {step}")
+
+
+def test_adam_and_norms_that_are_no_numbers(dgn):
+    f32 = [torch.float32]
+    g, p, m, v = (tensors([300, 40, 70], f32, seed=k) for k in range(4))
+    for t in v:
+        t.square_()
+    old = [[t.clone() for t in ts] for ts in (p, m, v)]
+    g[1][5] = float("nan")
+    lists = [dgn.TensorList(t) for t in (g, p, m, v)]
+    words = torch.tensor([1, 2, 3]).cuda()
+    b = dgn.GradientBuffers(lists[0], 2)
+    b.norm(words)
+    dgn.AdamBuffers(*lists).step(**ADAM, norms=b.norms, mask=words, skip_nonfinite=True)
+    for i in (1, 2):                                     # set 1 has the NaN, and tensor 2 as well
+        assert all(torch.equal(t[i], o[i]) for t, o in zip((p, m, v), old))
+    assert not torch.equal(p[0], old[0][0]) and p[0].isfinite().all()
+    dgn.AdamBuffers(*lists).step(**ADAM, norms=b.norms, mask=words)
+    assert p[1].isnan().all() and p[2].isnan().all() and p[0].isfinite().all()
+
+
+def test_empty_lists_and_empty_tensors(dgn):
+    for sizes in ([], [0], [0, 0, 0]):
+        g = tensors(sizes, [torch.float32])
+        lst = dgn.TensorList(g)
+        b = dgn.GradientBuffers(lst, 3)
+        b.norms.fill_(9.0)
+        b.norm()
+        assert (b.norms == 0).all()
+        b.clip(lst, 1.0)
+        dgn.AdamBuffers(lst, lst, lst, lst).step(**ADAM, norms=b.norms)
+    torch.cuda.synchronize()
+
+
+def test_many_tensors_and_one_large_one(dgn):
+    for sizes in ([7] * 3000, [3_000_001], [1, 2_000_003, 1]):
+        g = tensors(sizes, [torch.bfloat16])
+        words = words_of(len(g), 64)
+        b = dgn.GradientBuffers(dgn.TensorList(g), 64)
+        b.norm(words.cuda())
+        want = vo.norms(g, signed(words), 64)
+        assert ((b.norms.double().cpu() - want).abs() <= 2.0**-23 * want).all()
+
+
+def test_captured_graph_and_another_stream(dgn):
+    g, out = tensors(), tensors(seed=5)
+    lst, to = dgn.TensorList(g), dgn.TensorList(out)
+    f32 = [torch.float32]
+    p, m, v, q, r, s = (tensors(types=f32, seed=k) for k in range(6))
+    for t in v:
+        t.square_()
+    b = dgn.GradientBuffers(lst, 5)
+    a = dgn.AdamBuffers(lst, *(dgn.TensorList(t) for t in (p, m, v)), *(dgn.TensorList(t) for t in (q, r, s)))
+    words = words_of(len(g), 5).cuda()
+
+    def run(stream=None):
+        b.norm(words, stream=stream)
+        b.clip(to, 0.3, mask=words, stream=stream)
+        a.step(**ADAM, norms=b.norms, max_norm=0.3, mask=words, stream=stream)
+    run()
+    want = [t.clone() for ts in ([b.norms], out, q, r, s) for t in ts]
+    now = lambda: [t for ts in ([b.norms], out, q, r, s) for t in ts]  # noqa: E731
+    side = torch.cuda.Stream()
+    for t in now():
+        t.zero_()
+    torch.cuda.synchronize()
+    run(side)
+    side.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(want, now()))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for turn in range(4):
+        for t in now():
+            t.fill_(float(turn))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(want, now())), turn
+
+
+def test_refusals(dgn):
+    g = tensors()
+    lst = dgn.TensorList(g)
+    with pytest.raises(dgn.DgnError):
+        dgn.TensorList([g[0], torch.zeros(3)])                                   # another device
+    with pytest.raises(dgn.DgnError):
+        dgn.TensorList([torch.zeros(4, 4, device="cuda").t()])                   # not contiguous
+    with pytest.raises(dgn.DgnError):
+        dgn.TensorList([torch.zeros(4, device="cuda", dtype=torch.float64)])
+    b = dgn.GradientBuffers(lst)
+    few = torch.ones(len(g) - 1, dtype=torch.int64, device="cuda")
+    for kw in [dict(mask=few), dict(mask=few.int()), dict(ids=few.int()), dict(mask=few, ids=few.int())]:
+        with pytest.raises(dgn.DgnError):
+            b.norm(**kw)
+    for sets in (0, 65, -1):
+        with pytest.raises(dgn.DgnError):
+            dgn.GradientBuffers(lst, sets).norm()
+    f32 = [torch.float32]
+    other = dgn.TensorList(tensors(SIZES[:-1] + [70002], TYPES))
+    same = dgn.TensorList(tensors(types=f32))
+    for out, norm, eps in [(other, 1.0, 1e-6), (same, 1.0, 1e-6), (lst, -1.0, 1e-6), (lst, float("nan"), 1e-6), (lst, 1.0, -1.0)]:
+        with pytest.raises(dgn.DgnError):
+            b.clip(out, norm, eps=eps)
+    for lists in [(lst, lst, same, same), (lst, same, other, same), (lst, same, same, lst)]:
+        with pytest.raises(dgn.DgnError):
+            dgn.AdamBuffers(*lists).step(**ADAM)
+    ok = dgn.AdamBuffers(lst, same, same, same)
+    for bad in [dict(step=0), dict(beta1=1.0), dict(beta2=-0.1), dict(lr=float("nan")), dict(eps=-1.0), dict(weight_decay=-1.0)]:
+        with pytest.raises(dgn.DgnError):
+            ok.step(**{**ADAM, **bad})
+    with pytest.raises(dgn.DgnError):
+        ok.step(**ADAM, norms=b.norms, max_norm=-1.0)
+    with pytest.raises(dgn.DgnError):
+        ok.step(**ADAM, norms=b.norms.double())
+    lst.close()
+    with pytest.raises(dgn.DgnError):
+        b.norm()
