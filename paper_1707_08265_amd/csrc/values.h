@@ -8,21 +8,15 @@
 
 namespace dgn {
 
-// Element types in memory; arithmetic is in 32 bits throughout.
+// Element types in memory; arithmetic is in 32 bits throughout, conversions round to nearest, ties to even.
 struct F32 { typedef float Store; };
 struct F16 { typedef _Float16 Store; };
 struct BF16 { typedef __bf16 Store; };
 
-template <class T> __device__ __forceinline__ float to_float(typename T::Store v) { return (float)v; }
-template <class T> __device__ __forceinline__ typename T::Store from_float(float v) { return (typename T::Store)v; }   // nearest, ties to even
-
 inline int element_size(int32_t dtype) { return dtype == DGN_F32 ? 4 : 2; }
 
-// 1 / (1 + exp(-v)): without overflow for either sign, 0 and 1 at the infinities, NaN for NaN.
-__device__ __forceinline__ float sigmoid(float v) { return 1.0f / (1.0f + __expf(-v)); }
-
 // ---- gated linear recurrence --------------------------------------------------------------------
-constexpr int kScanTile = 128;      // tokens between two states that the forward pass keeps for the backward pass
+constexpr int kScanTile = 64;       // tokens between two states that the forward pass keeps for the backward pass
 struct ScanArgs {
     int64_t tokens, seqs, channels, group, heads;
     int64_t x_stride, gate_stride, y_stride, dy_stride, dx_stride, dgate_stride;
@@ -36,7 +30,11 @@ struct ScanArgs {
     const float *dfinal;
     void *dx, *dgate;
     float *dh0;
-    float *partial;                 // shared gates: a gate's gradient per channel, [tokens][channels]
+    // how rows and channels are cut, and scratch (set at the launch)
+    int64_t tiles, blocks, row_words;
+    int32_t width, parts;
+    u64 *ticket, *words;            // NULL: there is one tile
+    float *partial;                 // gates shared by more channels than a workgroup has: [parts][tokens][heads]
 };
 struct StepArgs {
     int64_t rows, slots, channels, group;
@@ -47,9 +45,9 @@ struct StepArgs {
     float *state_out;
     void *y;
 };
-size_t scan_scratch_bytes(int64_t tokens, int64_t channels, int64_t group);
-hipError_t launch_scan_forward(int dtype, int kind, const ScanArgs &a, hipStream_t s);
-hipError_t launch_scan_backward(int dtype, int kind, const ScanArgs &a, hipStream_t s);
+size_t scan_scratch_bytes(const ScanArgs &a);
+hipError_t launch_scan_forward(int dtype, int kind, ScanArgs a, void *scratch, hipStream_t s);
+hipError_t launch_scan_backward(int dtype, int kind, ScanArgs a, void *scratch, hipStream_t s);
 hipError_t launch_scan_step(int dtype, int kind, const StepArgs &a, hipStream_t s);
 
 // ---- lists of tensors -----------------------------------------------------------------------------

@@ -115,7 +115,7 @@ int dgn_scan_workspace(const dgn_scan_desc *d, size_t *scratch_bytes, size_t *ca
 {
     const int rc = check_scan(d);
     if (rc != DGN_OK) return rc;
-    if (scratch_bytes) *scratch_bytes = round256(scan_scratch_bytes(d->num_tokens, d->num_channels, d->gate_group));
+    if (scratch_bytes) *scratch_bytes = d->num_channels > 0 ? round256(scan_scratch_bytes(scan_args(d))) : 0;
     if (carry_bytes) *carry_bytes = round256((size_t)((d->num_tokens + kScanTile - 1) / kScanTile) * d->num_channels * 4);
     return DGN_OK;
 }
@@ -143,7 +143,7 @@ int dgn_scan_forward(const dgn_scan_desc *d, const void *x, const void *gate, co
     a.y = y;
     a.final = final;
     a.carry = static_cast<float *>(carry);
-    DGN_HIP(launch_scan_forward(d->dtype, d->gate_kind, a, static_cast<hipStream_t>(stream)));
+    DGN_HIP(launch_scan_forward(d->dtype, d->gate_kind, a, scratch, static_cast<hipStream_t>(stream)));
     return DGN_OK;
 }
 
@@ -176,8 +176,7 @@ int dgn_scan_backward(const dgn_scan_desc *d, const void *x, const void *gate, c
     a.dx = dx;
     a.dgate = dgate;
     a.dh0 = dh0;
-    a.partial = static_cast<float *>(scratch);
-    DGN_HIP(launch_scan_backward(d->dtype, d->gate_kind, a, static_cast<hipStream_t>(stream)));
+    DGN_HIP(launch_scan_backward(d->dtype, d->gate_kind, a, scratch, static_cast<hipStream_t>(stream)));
     return DGN_OK;
 }
 
