@@ -45,7 +45,7 @@ struct StepArgs {
     float *state_out;
     void *y;
 };
-size_t scan_scratch_bytes(const ScanArgs &a);
+size_t scan_scratch_bytes(int dtype, const ScanArgs &a);
 hipError_t launch_scan_forward(int dtype, int kind, ScanArgs a, void *scratch, hipStream_t s);
 hipError_t launch_scan_backward(int dtype, int kind, ScanArgs a, void *scratch, hipStream_t s);
 hipError_t launch_scan_step(int dtype, int kind, const StepArgs &a, hipStream_t s);

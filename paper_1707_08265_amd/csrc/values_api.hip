@@ -115,7 +115,7 @@ int dgn_scan_workspace(const dgn_scan_desc *d, size_t *scratch_bytes, size_t *ca
 {
     const int rc = check_scan(d);
     if (rc != DGN_OK) return rc;
-    if (scratch_bytes) *scratch_bytes = d->num_channels > 0 ? round256(scan_scratch_bytes(scan_args(d))) : 0;
+    if (scratch_bytes) *scratch_bytes = d->num_channels > 0 ? round256(scan_scratch_bytes(d->dtype, scan_args(d))) : 0;
     if (carry_bytes) *carry_bytes = round256((size_t)((d->num_tokens + kScanTile - 1) / kScanTile) * d->num_channels * 4);
     return DGN_OK;
 }
