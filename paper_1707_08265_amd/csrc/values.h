@@ -16,7 +16,7 @@ struct BF16 { typedef __bf16 Store; };
 inline int element_size(int32_t dtype) { return dtype == DGN_F32 ? 4 : 2; }
 
 // ---- gated linear recurrence --------------------------------------------------------------------
-constexpr int kScanTile = 64;       // tokens between two states that the forward pass keeps for the backward pass
+constexpr int kScanKeep = 16;       // rows between two states that the forward pass keeps for the backward pass
 struct ScanArgs {
     int64_t tokens, seqs, channels, group, heads;
     int64_t x_stride, gate_stride, y_stride, dy_stride, dx_stride, dgate_stride;
@@ -25,16 +25,17 @@ struct ScanArgs {
     const float *h0;
     void *y;
     float *final;
-    float *carry;                   // [ceil(tokens / kScanTile)][channels]: the state before the tile's first token
+    float *kept;                    // [ceil(tokens / kScanKeep)][channels]: the state before that row
     const void *dy;
     const float *dfinal;
     void *dx, *dgate;
     float *dh0;
-    // how rows and channels are cut, and scratch (set at the launch)
-    int64_t tiles, blocks, row_words;
+    // how rows and channels are cut (see gated_scan.hip), and scratch: set at the launch
+    int64_t strips, blocks, rows;
     int32_t width, parts;
-    u64 *ticket, *words;            // NULL: there is one tile
-    float *partial;                 // gates shared by more channels than a workgroup has: [parts][tokens][heads]
+    u64 *words;                     // [strips][blocks][64 V]: what a strip does to a state; NULL: there is one strip
+    float *states;                  // the same: the state that comes into it
+    float *partial;                 // gates shared by more channels than a wave has: [parts][tokens][heads]
 };
 struct StepArgs {
     int64_t rows, slots, channels, group;
@@ -45,9 +46,9 @@ struct StepArgs {
     float *state_out;
     void *y;
 };
+bool scan_fits(int dtype, const ScanArgs &a);
 size_t scan_scratch_bytes(int dtype, const ScanArgs &a);
-hipError_t launch_scan_forward(int dtype, int kind, ScanArgs a, void *scratch, hipStream_t s);
-hipError_t launch_scan_backward(int dtype, int kind, ScanArgs a, void *scratch, hipStream_t s);
+hipError_t launch_scan(int dtype, int kind, bool back, const ScanArgs &a, void *scratch, hipStream_t s);
 hipError_t launch_scan_step(int dtype, int kind, const StepArgs &a, hipStream_t s);
 
 // ---- lists of tensors -----------------------------------------------------------------------------

@@ -115,8 +115,9 @@ int dgn_scan_workspace(const dgn_scan_desc *d, size_t *scratch_bytes, size_t *ca
 {
     const int rc = check_scan(d);
     if (rc != DGN_OK) return rc;
+    if (d->num_channels > 0 && !scan_fits(d->dtype, scan_args(d))) return DGN_ERR_TOO_LARGE;
     if (scratch_bytes) *scratch_bytes = d->num_channels > 0 ? round256(scan_scratch_bytes(d->dtype, scan_args(d))) : 0;
-    if (carry_bytes) *carry_bytes = round256((size_t)((d->num_tokens + kScanTile - 1) / kScanTile) * d->num_channels * 4);
+    if (carry_bytes) *carry_bytes = round256((size_t)((d->num_tokens + kScanKeep - 1) / kScanKeep) * d->num_channels * 4);
     return DGN_OK;
 }
 
@@ -142,8 +143,8 @@ int dgn_scan_forward(const dgn_scan_desc *d, const void *x, const void *gate, co
     a.h0 = h0;
     a.y = y;
     a.final = final;
-    a.carry = static_cast<float *>(carry);
-    DGN_HIP(launch_scan_forward(d->dtype, d->gate_kind, a, scratch, static_cast<hipStream_t>(stream)));
+    a.kept = static_cast<float *>(carry);
+    DGN_HIP(launch_scan(d->dtype, d->gate_kind, false, a, scratch, static_cast<hipStream_t>(stream)));
     return DGN_OK;
 }
 
@@ -170,13 +171,13 @@ int dgn_scan_backward(const dgn_scan_desc *d, const void *x, const void *gate, c
     a.gate = gate;
     a.rowptr = seq_rowptr;
     a.h0 = h0;
-    a.carry = const_cast<float *>(static_cast<const float *>(carry));
+    a.kept = const_cast<float *>(static_cast<const float *>(carry));
     a.dy = dy;
     a.dfinal = dfinal;
     a.dx = dx;
     a.dgate = dgate;
     a.dh0 = dh0;
-    DGN_HIP(launch_scan_backward(d->dtype, d->gate_kind, a, scratch, static_cast<hipStream_t>(stream)));
+    DGN_HIP(launch_scan(d->dtype, d->gate_kind, true, a, scratch, static_cast<hipStream_t>(stream)));
     return DGN_OK;
 }
 
