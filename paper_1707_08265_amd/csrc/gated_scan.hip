@@ -184,7 +184,7 @@ template <int V, bool kShared> struct Strip {
     int64_t row0, c, head0;     // first row, first channel, and the head that has it
     int32_t rows, from, to;     // rows of it; those from `from` on, before `to`, belong to sequences
     int32_t part;
-    int64_t number;             // of the block
+    int64_t strip, number;      // and the number of the block
     uint32_t mine, head;        // the lane's place in the block, and its head's (32 bits: what is the same for the wave stays in scalar registers)
     bool active, last, marked, empties;
 
@@ -192,7 +192,7 @@ template <int V, bool kShared> struct Strip {
     __device__ __forceinline__ bool find(const ScanArgs &a, int64_t at, bool back)
     {
         if (at >= a.strips * a.blocks) return false;
-        int64_t strip = divide(at, a.blocks);
+        strip = divide(at, a.blocks);
         const int64_t strip_block = at - strip * a.blocks;
         const Block bl = block_of(a, strip_block);
         if (back) strip = a.strips - 1 - strip;
@@ -374,12 +374,29 @@ __global__ __launch_bounds__(kSlots *kPieces) void k_scan_states(const u64 *word
     s_link[piece][threadIdx.x % kSlots] = link_word(A, B, cut);
     __syncthreads();
     float h = 0.0f;
+#pragma unroll 8
     for (int p = 0; p < piece; p++) h = apply_word(s_link[p][threadIdx.x % kSlots], h);
 #pragma unroll 8
     for (int64_t n = from; n < to; n++) {
         const u64 w = words[row(n)];
         states[row(n)] = h;
         h = apply_word(w, h);
+    }
+}
+
+// The state that comes into a strip: the second launch has left it, or (few strips) the links before it are applied here.
+template <int V> __device__ __forceinline__ void state_before(const ScanArgs &a, int64_t strip, int64_t block, bool back, float (&h)[V])
+{
+    const int64_t slots = a.blocks * (kWave * V), at = block * (kWave * V) + lane_id() * V;
+#pragma unroll
+    for (int i = 0; i < V; i++) h[i] = a.states ? a.states[strip * slots + at + i] : 0.0f;
+    if (a.states) return;
+    const int n = (int)(back ? a.strips - 1 - strip : strip);
+#pragma unroll 4
+    for (int k = 0; k < n; k++) {
+        const u64 *w = a.words + (back ? a.strips - 1 - k : k) * slots + at;
+#pragma unroll
+        for (int i = 0; i < V; i++) h[i] = apply_word(w[i], h[i]);
     }
 }
 
@@ -394,7 +411,7 @@ __global__ __launch_bounds__(kStripWaves *kWave, 8) void k_scan_outputs(ScanArgs
     Strip<V, kShared> st;
     if (!st.find(a, (int64_t)blockIdx.x * kStripWaves + wave_id(), true)) return;
     float h[V];
-    load_state<V>(a.states ? a.states + (divide(st.row0, a.rows) * a.blocks + st.number) * (kWave * V) : nullptr, lane_id() * V, h);
+    state_before<V>(a, st.strip, st.number, false, h);
     st.mark(a, marks);
     if (st.empties && a.final) st.copy_empties(a, a.h0, a.final);
     S *y = static_cast<S *>(a.y) + st.row0 * a.y_stride + st.c;
@@ -463,7 +480,7 @@ __global__ __launch_bounds__(kStripWaves *kWave, 4) void k_scan_gradients(ScanAr
     Strip<V, kShared> st;
     if (!st.find(a, (int64_t)blockIdx.x * kStripWaves + wave_id(), true)) return;
     float e[V];
-    load_state<V>(a.states ? a.states + (divide(st.row0, a.rows) * a.blocks + st.number) * (kWave * V) : nullptr, lane_id() * V, e);
+    state_before<V>(a, st.strip, st.number, true, e);
     st.mark(a, marks);
     if (st.empties && a.dh0) st.copy_empties(a, a.dfinal, a.dh0);
     for (int k0 = (st.rows - 1) / kTokens * kTokens; k0 >= 0 && st.rows > 0; k0 -= kTokens) {
@@ -593,6 +610,7 @@ static int elements_of(int dtype, const ScanArgs &a, bool back)
 
 // Strips: as many as fill the waves of the card several times over (kStrips of them), of kKeep to kMostRows rows.
 constexpr int64_t kStrips = 8192;
+constexpr int64_t kFewStrips = 32;      // up to here a strip applies the links before it itself: 257 x 512 forward 14.9 us instead of 16.6
 struct Layout { int V; Cut cut; int64_t rows, strips; size_t words, states, partial, bytes; };
 static Layout lay_out(int dtype, const ScanArgs &a, bool back)
 {
@@ -631,18 +649,14 @@ static void scan_states(const ScanArgs &a, int V, bool back, hipStream_t s)
 }
 template <class T, int kKind, int V, bool kShared> static void go_forward(const ScanArgs &a, hipStream_t s)
 {
-    if (a.states) {
-        hipLaunchKernelGGL((k_scan_links<T, kKind, V, kShared, false>), grid_of(a), dim3(kStripWaves * kWave), 0, s, a);
-        scan_states(a, V, false, s);
-    }
+    if (a.strips > 1) hipLaunchKernelGGL((k_scan_links<T, kKind, V, kShared, false>), grid_of(a), dim3(kStripWaves * kWave), 0, s, a);
+    if (a.states) scan_states(a, V, false, s);
     hipLaunchKernelGGL((k_scan_outputs<T, kKind, V, kShared>), grid_of(a), dim3(kStripWaves * kWave), 0, s, a);
 }
 template <class T, int kKind, int V, bool kShared> static void go_backward(const ScanArgs &a, hipStream_t s)
 {
-    if (a.states) {
-        hipLaunchKernelGGL((k_scan_links<T, kKind, V, kShared, true>), grid_of(a), dim3(kStripWaves * kWave), 0, s, a);
-        scan_states(a, V, true, s);
-    }
+    if (a.strips > 1) hipLaunchKernelGGL((k_scan_links<T, kKind, V, kShared, true>), grid_of(a), dim3(kStripWaves * kWave), 0, s, a);
+    if (a.states) scan_states(a, V, true, s);
     hipLaunchKernelGGL((k_scan_gradients<T, kKind, V, kShared>), grid_of(a), dim3(kStripWaves * kWave), 0, s, a);
     if (a.parts > 1 && a.tokens > 0) {
         const int64_t n = (a.tokens * a.heads + 255) / 256;
@@ -659,10 +673,8 @@ template <class T, int kKind> static hipError_t go(int dtype, bool back, ScanArg
     a.rows = l.rows;
     a.strips = l.strips;
     a.partial = reinterpret_cast<float *>(mem + l.partial);
-    if (a.strips > 1) {
-        a.words = reinterpret_cast<u64 *>(mem + l.words);
-        a.states = reinterpret_cast<float *>(mem + l.states);
-    }
+    a.words = reinterpret_cast<u64 *>(mem + l.words);
+    if (a.strips > kFewStrips) a.states = reinterpret_cast<float *>(mem + l.states);
     constexpr bool kWide = sizeof(typename T::Store) == 4;
     constexpr int kForward = kWide ? 2 : 4, kBackward = kWide ? 1 : 2;      // elements of a lane, at most
     if (a.group == 1) {

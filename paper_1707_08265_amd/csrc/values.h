@@ -33,8 +33,8 @@ struct ScanArgs {
     // how rows and channels are cut (see gated_scan.hip), and scratch: set at the launch
     int64_t strips, blocks, rows;
     int32_t width, parts;
-    u64 *words;                     // [strips][blocks][64 V]: what a strip does to a state; NULL: there is one strip
-    float *states;                  // the same: the state that comes into it
+    u64 *words;                     // [strips][blocks][64 V]: what a strip does to a state
+    float *states;                  // the same: the state that comes into it; NULL: few strips
     float *partial;                 // gates shared by more channels than a wave has: [parts][tokens][heads]
 };
 struct StepArgs {
