@@ -141,12 +141,6 @@ constexpr int kStripWaves = 4;          // waves of a workgroup; each has a stri
 struct Marks {
     int32_t begin[kMostRows], end[kMostRows];       // the sequence whose first / last row this is, or -1
 };
-__device__ __forceinline__ void wave_fence()
-{
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
 // Number of rowptr[0 .. n-1] below `value`; one wave, 64 looks at a time.
 __device__ __forceinline__ int64_t rows_below(const int64_t *rowptr, int64_t n, int64_t value)
 {

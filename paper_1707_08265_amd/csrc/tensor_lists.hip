@@ -11,18 +11,92 @@ __device__ __forceinline__ double wave_sum_double(double v)
     return v;
 }
 
-__device__ __forceinline__ float load_at(const void *p, int dtype, int64_t i)
+// N neighbouring elements, at an address that is aligned to one, in 32 bits.
+typedef uint32_t Quad32 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t Quad16 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t Pair16 __attribute__((ext_vector_type(2), aligned(2)));
+template <class T> __device__ __forceinline__ float half_of(uint32_t w, int i)
 {
-    if (dtype == DGN_F32) return static_cast<const float *>(p)[i];
-    if (dtype == DGN_F16) return (float)static_cast<const _Float16 *>(p)[i];
-    return (float)static_cast<const __bf16 *>(p)[i];
+    return (float)__builtin_bit_cast(typename T::Store, (uint16_t)(w >> (16 * i)));
 }
-__device__ __forceinline__ void store_at(void *p, int dtype, int64_t i, float v)
+template <class T> __device__ __forceinline__ uint32_t two_halves(float a, float b)
 {
-    if (dtype == DGN_F32) static_cast<float *>(p)[i] = v;
-    else if (dtype == DGN_F16) static_cast<_Float16 *>(p)[i] = (_Float16)v;
-    else static_cast<__bf16 *>(p)[i] = (__bf16)v;
+    typedef typename T::Store H2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, H2{(typename T::Store)a, (typename T::Store)b});
 }
+// What a thread takes of a tensor at a time: sixteen bytes.
+template <class T> struct Run;
+template <> struct Run<F32> {
+    static constexpr int kN = 4;
+    Quad32 w;
+    __device__ __forceinline__ void load(const float *p) { w = *reinterpret_cast<const Quad32 *>(p); }
+    __device__ __forceinline__ void store(float *p) const { *reinterpret_cast<Quad32 *>(p) = w; }
+    __device__ __forceinline__ float get(int i) const { return __uint_as_float(w[i]); }
+    __device__ __forceinline__ void scale(float f)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; i++) w[i] = __float_as_uint(get(i) * f);
+    }
+};
+template <class T> struct Run16 {
+    typedef typename T::Store S;
+    static constexpr int kN = 8;
+    Quad16 w;
+    __device__ __forceinline__ void load(const S *p) { w = *reinterpret_cast<const Quad16 *>(p); }
+    __device__ __forceinline__ void store(S *p) const { *reinterpret_cast<Quad16 *>(p) = w; }
+    __device__ __forceinline__ float get(int i) const { return half_of<T>(w[i / 2], i % 2); }
+    __device__ __forceinline__ void scale(float f)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; i++) w[i] = two_halves<T>(get(2 * i) * f, get(2 * i + 1) * f);
+    }
+};
+template <> struct Run<F16> : Run16<F16> {};
+template <> struct Run<BF16> : Run16<BF16> {};
+// Four elements of any type.
+template <class T> struct Four;
+template <> struct Four<F32> {
+    static __device__ __forceinline__ void load(const float *p, float (&f)[4])
+    {
+        const Quad32 w = *reinterpret_cast<const Quad32 *>(p);
+#pragma unroll
+        for (int i = 0; i < 4; i++) f[i] = __uint_as_float(w[i]);
+    }
+    static __device__ __forceinline__ void store(float *p, const float (&f)[4])
+    {
+        *reinterpret_cast<Quad32 *>(p) = Quad32{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+    }
+};
+template <class T> struct Four16 {
+    typedef typename T::Store S;
+    static __device__ __forceinline__ void load(const S *p, float (&f)[4])
+    {
+        const Pair16 w = *reinterpret_cast<const Pair16 *>(p);
+#pragma unroll
+        for (int i = 0; i < 4; i++) f[i] = half_of<T>(w[i / 2], i % 2);
+    }
+    static __device__ __forceinline__ void store(S *p, const float (&f)[4])
+    {
+        *reinterpret_cast<Pair16 *>(p) = Pair16{two_halves<T>(f[0], f[1]), two_halves<T>(f[2], f[3])};
+    }
+};
+template <> struct Four<F16> : Four16<F16> {};
+template <> struct Four<BF16> : Four16<BF16> {};
+
+// A chunk's own elements: where they begin, and how many there are.
+struct Part { int32_t entry; int64_t from; int32_t n; };
+__device__ __forceinline__ Part part_of(const ListView &l, int32_t chunk)
+{
+    const ListChunk c = l.chunk[chunk];
+    const int64_t from = (int64_t)c.index * kListChunk, left = l.entry[c.entry].numel - from;
+    return Part{c.entry, from, (int32_t)(left < kListChunk ? left : kListChunk)};
+}
+#define DGN_BY_DTYPE(dtype, call)                 \
+    do {                                          \
+        if ((dtype) == DGN_F32) { call(F32); }    \
+        else if ((dtype) == DGN_F16) { call(F16); } \
+        else { call(BF16); }                      \
+    } while (0)
 
 // The sets that reach an entry: its word of the mask, or that of the tensor that it stands for (none, if there is no such
 // tensor); without a mask every set does.
@@ -34,46 +108,88 @@ __device__ __forceinline__ u64 reach_of(const Reach &r, int32_t entry)
     return at >= 0 && at < r.words ? r.mask[at] & all : 0;
 }
 
+constexpr int kListThreads = 256;
+
 // Squares are added up in 64 bits: those of 32-bit gradients above 2e19 or below 1e-23 have no 32-bit value.
-__global__ __launch_bounds__(256) void k_list_squares(ListView g, double *partial)
+template <class T> __device__ __forceinline__ double squares(const typename T::Store *p, int n)
 {
-    __shared__ double s_sum[4];
-    const ListChunk c = g.chunk[blockIdx.x];
-    const ListEntry e = g.entry[c.entry];
-    const int64_t from = (int64_t)c.index * kListChunk, to = from + kListChunk < e.numel ? from + kListChunk : e.numel;
-    double sum = 0.0;
-    for (int64_t i = from + threadIdx.x; i < to; i += 256) {
-        const double v = load_at(e.data, e.dtype, i);
-        sum += v * v;
+    constexpr int kN = Run<T>::kN, kTurn = kListThreads * kN, kAhead = 4;
+    double sum[2] = {0.0, 0.0};
+    int i = threadIdx.x * kN;
+    for (; i + (kAhead - 1) * kTurn + kN <= n; i += kAhead * kTurn) {
+        Run<T> r[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) r[u].load(p + i + u * kTurn);
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) {
+#pragma unroll
+            for (int k = 0; k < kN; k++) { const double v = r[u].get(k); sum[k % 2] = fma(v, v, sum[k % 2]); }
+        }
     }
+    for (; i + kN <= n; i += kTurn) {
+        Run<T> r;
+        r.load(p + i);
+#pragma unroll
+        for (int k = 0; k < kN; k++) { const double v = r.get(k); sum[k % 2] = fma(v, v, sum[k % 2]); }
+    }
+    i = n / kN * kN + threadIdx.x;
+    if (i < n) { const double v = (float)p[i]; sum[0] = fma(v, v, sum[0]); }
+    return sum[0] + sum[1];
+}
+__global__ __launch_bounds__(kListThreads) void k_list_squares(ListView g, double *partial, uint32_t *arrived)
+{
+    __shared__ double s_sum[kListThreads / kWave];
+    const Part part = part_of(g, blockIdx.x);
+    const ListEntry e = g.entry[part.entry];
+    double sum = 0.0;
+#define DGN_GO(T) sum = squares<T>(static_cast<const typename T::Store *>(e.data) + part.from, part.n)
+    DGN_BY_DTYPE(e.dtype, DGN_GO);
+#undef DGN_GO
     sum = wave_sum_double(sum);
     if (lane_id() == 0) s_sum[threadIdx.x >> 6] = sum;
     __syncthreads();
-    if (threadIdx.x == 0) partial[blockIdx.x] = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
+    if (threadIdx.x == 0) {
+        partial[blockIdx.x] = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
+        if (blockIdx.x == 0) *arrived = 0;              // for the next launch
+    }
 }
 
-// A lane per set; the chunks in a fixed order, so the same gradients give the same norms.
-__global__ __launch_bounds__(1024) void k_list_norms(ListView g, Reach r, const double *partial, float *norms)
+// The chunks' sums to the sets': a lane per set, kPerGroup chunks to a workgroup, and the workgroups' sums by the one that is done last.
+// Always in the same order, so the same gradients give the same norms.
+constexpr int kPerGroup = 256;
+__global__ __launch_bounds__(kListThreads) void k_list_norms(ListView g, Reach r, const double *partial, double *sums, uint32_t *arrived, float *norms)
 {
-    __shared__ double s_sum[16][kWave];
+    struct Link { double sum; u64 bits; };
+    __shared__ Link s_link[kPerGroup];
+    __shared__ double s_sum[kListThreads / kWave][kWave];
+    __shared__ bool s_last;
     const int lane = lane_id(), wave = threadIdx.x >> 6;
+    const int32_t chunk = blockIdx.x * kPerGroup + threadIdx.x;
+    const bool some = chunk < g.chunks;
+    s_link[threadIdx.x] = Link{some ? partial[chunk] : 0.0, some ? reach_of(r, g.chunk[chunk].entry) : 0};
+    __syncthreads();
     double sum = 0.0;
-    for (int32_t at = wave * kWave; at < g.chunks; at += 1024) {
-        const bool some = at + lane < g.chunks;
-        const double v = some ? partial[at + lane] : 0.0;
-        const u64 bits = some ? reach_of(r, g.chunk[at + lane].entry) : 0;
-        for (int j = 0; j < kWave; j++) {
-            const double w = __shfl(v, j, kWave);
-            if (shfl64(bits, j) >> lane & 1) sum += w;
-        }
+#pragma unroll 4
+    for (int j = 0; j < kWave; j++) {
+        const Link l = s_link[wave * kWave + j];
+        if (l.bits >> lane & 1) sum += l.sum;           // (what a set does not need does not count, whatever it is)
     }
     s_sum[wave][lane] = sum;
     __syncthreads();
-    if (wave == 0 && lane < r.sets) {
+    if (wave != 0) return;
+    sum = (s_sum[0][lane] + s_sum[1][lane]) + (s_sum[2][lane] + s_sum[3][lane]);
+    if (gridDim.x > 1) {
+        store_coherent(reinterpret_cast<u64 *>(sums) + blockIdx.x * kWave + lane, (u64)__double_as_longlong(sum));
+        __threadfence();
+        if (lane == 0) s_last = atomicAdd(arrived, 1u) == gridDim.x - 1;
+        wave_fence();
+        if (!s_last) return;
+        __threadfence();
         sum = 0.0;
-        for (int w = 0; w < 16; w++) sum += s_sum[w][lane];
-        norms[lane] = (float)sqrt(sum);
+#pragma unroll 8
+        for (unsigned b = 0; b < gridDim.x; b++) sum += __longlong_as_double((long long)load_coherent(reinterpret_cast<const u64 *>(sums) + b * kWave + lane));
     }
+    if (lane < r.sets) norms[lane] = (float)sqrt(sum);
 }
 
 // The least factor of the sets that reach a tensor (NaN if one of their norms is), 1 where none does.
@@ -97,61 +213,135 @@ __device__ __forceinline__ float clip_factor(const ClipArgs &c, u64 bits, bool &
     return f;
 }
 
-__global__ __launch_bounds__(256) void k_list_clip(ListView g, ListView out, ClipArgs cl)
+template <class T> __device__ __forceinline__ void scale_to(typename T::Store *out, const typename T::Store *p, int n, float f)
 {
-    const ListChunk c = g.chunk[blockIdx.x];
-    const ListEntry e = g.entry[c.entry], o = out.entry[c.entry];
+    constexpr int kN = Run<T>::kN, kTurn = kListThreads * kN, kAhead = 4;
+    int i = threadIdx.x * kN;
+    for (; i + (kAhead - 1) * kTurn + kN <= n; i += kAhead * kTurn) {
+        Run<T> r[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) r[u].load(p + i + u * kTurn);
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) {
+            if (f != 1.0f) r[u].scale(f);
+            r[u].store(out + i + u * kTurn);
+        }
+    }
+    for (; i + kN <= n; i += kTurn) {
+        Run<T> r;
+        r.load(p + i);
+        if (f != 1.0f) r.scale(f);
+        r.store(out + i);
+    }
+    i = n / kN * kN + threadIdx.x;
+    if (i < n) out[i] = f != 1.0f ? (typename T::Store)((float)p[i] * f) : p[i];
+}
+// The chunks from the last to the first: what the norms' pass read last is still in the cache.
+__global__ __launch_bounds__(kListThreads) void k_list_clip(ListView g, ListView out, ClipArgs cl)
+{
+    const Part part = part_of(g, gridDim.x - 1 - blockIdx.x);
+    const ListEntry e = g.entry[part.entry], o = out.entry[part.entry];
     bool finite;
-    const float f = clip_factor(cl, reach_of(cl.reach, c.entry), finite);
+    const float f = clip_factor(cl, reach_of(cl.reach, part.entry), finite);
     if (f == 1.0f && e.data == o.data) return;
-    const int64_t from = (int64_t)c.index * kListChunk, to = from + kListChunk < e.numel ? from + kListChunk : e.numel;
-    for (int64_t i = from + threadIdx.x; i < to; i += 256) store_at(o.data, o.dtype, i, load_at(e.data, e.dtype, i) * f);
+#define DGN_GO(T) scale_to<T>(static_cast<typename T::Store *>(o.data) + part.from, static_cast<const typename T::Store *>(e.data) + part.from, part.n, f)
+    DGN_BY_DTYPE(e.dtype, DGN_GO);
+#undef DGN_GO
 }
 
-__global__ __launch_bounds__(256) void k_list_adam(AdamArgs a)
+struct AdamRow { const float *p, *m, *v; float *op, *om, *ov; };
+__device__ __forceinline__ void adam_one(const AdamArgs &a, float g, float &p, float &m, float &v)
 {
-    const ListChunk c = a.grad.chunk[blockIdx.x];
-    const ListEntry g = a.grad.entry[c.entry];
-    const u64 bits = reach_of(a.clip.reach, c.entry);
+    m = a.beta1 * m + a.rest1 * g;
+    v = a.beta2 * v + a.rest2 * (g * g);
+    p -= a.decay * p + a.rate * m / (sqrtf(v * a.spread) + a.eps);
+}
+template <class T>
+__device__ __forceinline__ void adam_chunk(const AdamArgs &a, const typename T::Store *g, const AdamRow &r, void *copy, int32_t copy_type, int n,
+                                           float f, bool live)
+{
+    constexpr int kTurn = kListThreads * 4;
+    for (int i = threadIdx.x * 4; i + 4 <= n; i += kTurn) {
+        float d[4], p[4], m[4], v[4];
+        Four<T>::load(g + i, d);
+        Four<F32>::load(r.p + i, p);
+        Four<F32>::load(r.m + i, m);
+        Four<F32>::load(r.v + i, v);
+        if (live) {
+#pragma unroll
+            for (int k = 0; k < 4; k++) adam_one(a, d[k] * f, p[k], m[k], v[k]);
+        }
+        Four<F32>::store(r.op + i, p);
+        Four<F32>::store(r.om + i, m);
+        Four<F32>::store(r.ov + i, v);
+        if (copy) {
+#define DGN_GO(C) Four<C>::store(static_cast<typename C::Store *>(copy) + i, p)
+            DGN_BY_DTYPE(copy_type, DGN_GO);
+#undef DGN_GO
+        }
+    }
+    const int i = n / 4 * 4 + threadIdx.x;
+    if (i < n) {
+        float p = r.p[i], m = r.m[i], v = r.v[i];
+        if (live) adam_one(a, (float)g[i] * f, p, m, v);
+        r.op[i] = p;
+        r.om[i] = m;
+        r.ov[i] = v;
+        if (copy) {
+#define DGN_GO(C) static_cast<typename C::Store *>(copy)[i] = (typename C::Store)p
+            DGN_BY_DTYPE(copy_type, DGN_GO);
+#undef DGN_GO
+        }
+    }
+}
+__global__ __launch_bounds__(kListThreads) void k_list_adam(AdamArgs a)
+{
+    const Part part = part_of(a.grad, gridDim.x - 1 - blockIdx.x);
+    const ListEntry g = a.grad.entry[part.entry];
+    const u64 bits = reach_of(a.clip.reach, part.entry);
     bool finite = true;
     const float f = a.clip.norms ? clip_factor(a.clip, bits, finite) : 1.0f;
     const bool live = bits != 0 && (finite || !a.skip_nonfinite);
-    const float *p = static_cast<const float *>(a.param.entry[c.entry].data), *m = static_cast<const float *>(a.m.entry[c.entry].data),
-                *v = static_cast<const float *>(a.v.entry[c.entry].data);
-    float *op = static_cast<float *>(a.out_param.entry[c.entry].data), *om = static_cast<float *>(a.out_m.entry[c.entry].data),
-          *ov = static_cast<float *>(a.out_v.entry[c.entry].data);
-    const int64_t from = (int64_t)c.index * kListChunk, to = from + kListChunk < g.numel ? from + kListChunk : g.numel;
-    for (int64_t i = from + threadIdx.x; i < to; i += 256) {
-        float np = p[i], nm = m[i], nv = v[i];
-        if (live) {
-            const float d = load_at(g.data, g.dtype, i) * f;
-            nm = a.beta1 * nm + a.rest1 * d;
-            nv = a.beta2 * nv + a.rest2 * (d * d);
-            np -= a.decay * np + a.rate * nm / (sqrtf(nv * a.spread) + a.eps);
-        }
-        op[i] = np;
-        om[i] = nm;
-        ov[i] = nv;
-        if (a.copy.entries) store_at(a.copy.entry[c.entry].data, a.copy.entry[c.entry].dtype, i, np);
-    }
+    const auto at = [&](const ListView &l) { return static_cast<float *>(l.entry[part.entry].data) + part.from; };
+    const AdamRow r = {at(a.param), at(a.m), at(a.v), at(a.out_param), at(a.out_m), at(a.out_v)};
+    void *copy = nullptr;
+    int32_t copy_type = DGN_F32;
+    if (a.copy.entries) {
+        const ListEntry c = a.copy.entry[part.entry];
+        copy_type = c.dtype;
+        copy = static_cast<char *>(c.data) + part.from * (copy_type == DGN_F32 ? 4 : 2);
+    } else if (!live && r.p == r.op && r.m == r.om && r.v == r.ov) return;
+#define DGN_GO(T) adam_chunk<T>(a, static_cast<const typename T::Store *>(g.data) + part.from, r, copy, copy_type, part.n, f, live)
+    DGN_BY_DTYPE(g.dtype, DGN_GO);
+#undef DGN_GO
 }
 
-hipError_t launch_list_norms(const ListView &g, const Reach &r, double *partial, float *norms, hipStream_t s)
+// Scratch of the norms: a sum per chunk, the workgroups' sums for each set, and how many of them are done.
+static int norm_groups(const ListView &g) { return (g.chunks + kPerGroup - 1) / kPerGroup; }
+size_t list_norms_scratch_bytes(const ListView &g)
 {
-    if (g.chunks > 0) hipLaunchKernelGGL(k_list_squares, dim3((unsigned)g.chunks), dim3(256), 0, s, g, partial);
-    hipLaunchKernelGGL(k_list_norms, dim3(1), dim3(1024), 0, s, g, r, partial, norms);
+    return sizeof(double) * ((size_t)g.chunks + (size_t)norm_groups(g) * kWave) + 256;
+}
+
+hipError_t launch_list_norms(const ListView &g, const Reach &r, void *scratch, float *norms, hipStream_t s)
+{
+    double *partial = static_cast<double *>(scratch), *sums = partial + g.chunks;
+    const int groups = norm_groups(g);
+    uint32_t *arrived = reinterpret_cast<uint32_t *>(sums + (size_t)groups * kWave);
+    if (g.chunks > 0) hipLaunchKernelGGL(k_list_squares, dim3((unsigned)g.chunks), dim3(kListThreads), 0, s, g, partial, arrived);
+    hipLaunchKernelGGL(k_list_norms, dim3((unsigned)(groups > 0 ? groups : 1)), dim3(kListThreads), 0, s, g, r, partial, sums, arrived, norms);
     return hipGetLastError();
 }
 
 hipError_t launch_list_clip(const ListView &g, const ListView &out, const ClipArgs &c, hipStream_t s)
 {
-    if (g.chunks > 0) hipLaunchKernelGGL(k_list_clip, dim3((unsigned)g.chunks), dim3(256), 0, s, g, out, c);
+    if (g.chunks > 0) hipLaunchKernelGGL(k_list_clip, dim3((unsigned)g.chunks), dim3(kListThreads), 0, s, g, out, c);
     return hipGetLastError();
 }
 
 hipError_t launch_list_adam(const AdamArgs &a, hipStream_t s)
 {
-    if (a.grad.chunks > 0) hipLaunchKernelGGL(k_list_adam, dim3((unsigned)a.grad.chunks), dim3(256), 0, s, a);
+    if (a.grad.chunks > 0) hipLaunchKernelGGL(k_list_adam, dim3((unsigned)a.grad.chunks), dim3(kListThreads), 0, s, a);
     return hipGetLastError();
 }
 

@@ -15,6 +15,13 @@ struct BF16 { typedef __bf16 Store; };
 
 inline int element_size(int32_t dtype) { return dtype == DGN_F32 ? 4 : 2; }
 
+// What lanes of a wave wrote to LDS is there for the others.
+__device__ __forceinline__ void wave_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // ---- gated linear recurrence --------------------------------------------------------------------
 constexpr int kScanKeep = 16;       // rows between two states that the forward pass keeps for the backward pass
 struct ScanArgs {
@@ -66,7 +73,8 @@ struct AdamArgs {
     float spread;                                                   // 1 / (1 - beta2^t)
     int32_t skip_nonfinite;
 };
-hipError_t launch_list_norms(const ListView &g, const Reach &r, double *partial, float *norms, hipStream_t s);
+size_t list_norms_scratch_bytes(const ListView &g);
+hipError_t launch_list_norms(const ListView &g, const Reach &r, void *scratch, float *norms, hipStream_t s);
 hipError_t launch_list_clip(const ListView &g, const ListView &out, const ClipArgs &c, hipStream_t s);
 hipError_t launch_list_adam(const AdamArgs &a, hipStream_t s);
 

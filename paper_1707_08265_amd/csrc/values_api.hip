@@ -272,7 +272,7 @@ void dgn_list_destroy(dgn_list *l)
 int dgn_list_norms_workspace(const dgn_list *l, size_t *scratch_bytes)
 {
     if (!l || !scratch_bytes) return DGN_ERR_NULL_PTR;
-    *scratch_bytes = round256(sizeof(double) * (size_t)l->v.chunks) + 256;
+    *scratch_bytes = round256(list_norms_scratch_bytes(l->v));
     return DGN_OK;
 }
 
@@ -287,7 +287,7 @@ int dgn_list_norms(const dgn_list *l, const dgn_reach *reach, float *norms, void
     if (rc != DGN_OK) return rc;
     if (scratch_bytes < need) return DGN_ERR_WORKSPACE_TOO_SMALL;
     if (misaligned(scratch, 8) || misaligned(norms, 4)) return DGN_ERR_INVALID_ARG;
-    DGN_HIP(launch_list_norms(l->v, r, static_cast<double *>(scratch), norms, static_cast<hipStream_t>(stream)));
+    DGN_HIP(launch_list_norms(l->v, r, scratch, norms, static_cast<hipStream_t>(stream)));
     return DGN_OK;
 }
 
