@@ -507,7 +507,7 @@ typedef struct dgn_list_desc {
     const int32_t *dtype;    /* HOST [count]                                                */
 } dgn_list_desc;
 int dgn_list_workspace(const dgn_list_desc *desc, size_t *list_bytes);
-/* list_mem: DEVICE, 8-byte aligned, lives as long as the handle.  Synchronises the stream. */
+/* list_mem: DEVICE, 16-byte aligned, lives as long as the handle.  Synchronises the stream. */
 int dgn_list_build(const dgn_list_desc *desc, void *list_mem, size_t list_bytes, dgn_stream stream, dgn_list **out);
 void dgn_list_destroy(dgn_list *list);
 

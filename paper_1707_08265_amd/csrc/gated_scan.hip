@@ -38,6 +38,7 @@ __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane
 
 typedef uint32_t Word __attribute__((aligned(2)));
 typedef uint32_t Pair __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t Quad4 __attribute__((ext_vector_type(4), aligned(4)));
 
 // V neighbouring elements, at an address that is aligned to one, as they are in memory.
 template <class T, int V> struct Pack {
@@ -48,13 +49,19 @@ template <class T, int V> struct Pack {
     {
         if (kBytes == 2) w[0] = *reinterpret_cast<const uint16_t *>(p);
         else if (kBytes == 4) w[0] = *reinterpret_cast<const Word *>(p);
-        else { const Pair v = *reinterpret_cast<const Pair *>(p); w[0] = v[0]; w[kWords - 1] = v[1]; }
+        else if (kBytes == 8) { const Pair v = *reinterpret_cast<const Pair *>(p); w[0] = v[0]; w[1 % kWords] = v[1]; }
+        else {
+            const Quad4 v = *reinterpret_cast<const Quad4 *>(p);
+#pragma unroll
+            for (int i = 0; i < 4; i++) w[i % kWords] = v[i];
+        }
     }
     __device__ __forceinline__ void store(S *p) const
     {
         if (kBytes == 2) *reinterpret_cast<uint16_t *>(p) = (uint16_t)w[0];
         else if (kBytes == 4) *reinterpret_cast<Word *>(p) = w[0];
-        else *reinterpret_cast<Pair *>(p) = Pair{w[0], w[kWords - 1]};
+        else if (kBytes == 8) *reinterpret_cast<Pair *>(p) = Pair{w[0], w[1 % kWords]};
+        else *reinterpret_cast<Quad4 *>(p) = Quad4{w[0], w[1 % kWords], w[2 % kWords], w[3 % kWords]};
     }
     __device__ __forceinline__ float get(int i) const
     {
@@ -574,22 +581,36 @@ __global__ __launch_bounds__(256) void k_gate_sums(ScanArgs a)
     }
 }
 
-template <class T, int kKind>
+// One token: a row of the batch is cut into pieces of 256 V channels, a workgroup each.
+template <class T, int kKind, int V, bool kShared>
 __global__ __launch_bounds__(256) void k_scan_step(StepArgs a)
 {
     typedef typename T::Store S;
-    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (c >= a.channels) return;
-    for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
-    const int64_t slot = a.slot ? a.slot[row] : row;
-    float h = 0.0f;
-    if (slot >= 0 && slot < a.slots) {
-        float g, b;
-        open_gate<kKind>((float)(static_cast<const S *>(a.gate)[row * a.gate_stride + c / a.group]), g, b);
-        h = g * a.state_in[slot * a.channels + c] + b * (float)(static_cast<const S *>(a.x)[row * a.x_stride + c]);
-        a.state_out[slot * a.channels + c] = h;
-    }
-    static_cast<S *>(a.y)[row * a.y_stride + c] = (S)h;
+    for (int64_t at = blockIdx.x; at < a.rows * a.pieces; at += gridDim.x) {
+        const int64_t row = divide(at, a.pieces), c = (at - row * a.pieces) * (256 * V) + threadIdx.x * V;
+        if (c >= a.channels) continue;
+        const int64_t slot = a.slot ? a.slot[row] : row;
+        Pack<T, V> x, y;
+        Pack<T, kShared ? 1 : V> g;
+        x.load(static_cast<const S *>(a.x) + row * a.x_stride + c);
+        g.load(static_cast<const S *>(a.gate) + row * a.gate_stride + (kShared ? c / a.group : c));
+        float h[V];
+#pragma unroll
+        for (int i = 0; i < V; i++) h[i] = 0.0f;
+        if (slot >= 0 && slot < a.slots) {
+            Pack<F32, V> state;
+            state.load(a.state_in + slot * a.channels + c);
+            float ga, gb;
+#pragma unroll
+            for (int i = 0; i < V; i++) {
+                if (!kShared || i == 0) open_gate<kKind>(g.get(i), ga, gb);
+                h[i] = fmaf(ga, state.get(i), gb * x.get(i));
+            }
+            state.set(h);
+            state.store(a.state_out + slot * a.channels + c);
+        }
+        y.set(h);
+        y.store(static_cast<S *>(a.y) + row * a.y_stride + c);
     }
 }
 
@@ -699,11 +720,23 @@ hipError_t launch_scan(int dtype, int kind, bool back, const ScanArgs &a, void *
 #undef DGN_GO
 }
 
+template <class T, int kKind> static void go_step(StepArgs a, hipStream_t s)
+{
+    const int V = (a.group == 1 ? a.channels : a.group) % 4 == 0 ? 4 : 1;
+    a.pieces = (a.channels + 256 * V - 1) / (256 * V);
+    const int64_t n = a.rows * a.pieces;
+    const dim3 grid((unsigned)(n < (1 << 22) ? n : 1 << 22));
+    if (a.group == 1) {
+        if (V == 4) hipLaunchKernelGGL((k_scan_step<T, kKind, 4, false>), grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((k_scan_step<T, kKind, 1, false>), grid, dim3(256), 0, s, a);
+    } else {
+        if (V == 4) hipLaunchKernelGGL((k_scan_step<T, kKind, 4, true>), grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((k_scan_step<T, kKind, 1, true>), grid, dim3(256), 0, s, a);
+    }
+}
 hipError_t launch_scan_step(int dtype, int kind, const StepArgs &a, hipStream_t s)
 {
-    if (a.channels == 0 || a.rows == 0) return hipSuccess;
-    const dim3 grid((unsigned)((a.channels + 255) / 256), (unsigned)(a.rows < 32768 ? a.rows : 32768));
-#define DGN_GO(T, K) hipLaunchKernelGGL((k_scan_step<T, K>), grid, dim3(256), 0, s, a)
+#define DGN_GO(T, K) go_step<T, K>(a, s)
     DGN_BY_TYPE(DGN_GO);
 #undef DGN_GO
     return hipGetLastError();

@@ -83,14 +83,8 @@ template <class T> struct Four16 {
 template <> struct Four<F16> : Four16<F16> {};
 template <> struct Four<BF16> : Four16<BF16> {};
 
-// A chunk's own elements: where they begin, and how many there are.
-struct Part { int32_t entry; int64_t from; int32_t n; };
-__device__ __forceinline__ Part part_of(const ListView &l, int32_t chunk)
-{
-    const ListChunk c = l.chunk[chunk];
-    const int64_t from = (int64_t)c.index * kListChunk, left = l.entry[c.entry].numel - from;
-    return Part{c.entry, from, (int32_t)(left < kListChunk ? left : kListChunk)};
-}
+__device__ __forceinline__ int elements(const ListChunk &c) { return (int)(c.n_type >> 2); }
+__device__ __forceinline__ int type(const ListChunk &c) { return (int)(c.n_type & 3); }
 #define DGN_BY_DTYPE(dtype, call)                 \
     do {                                          \
         if ((dtype) == DGN_F32) { call(F32); }    \
@@ -111,11 +105,11 @@ __device__ __forceinline__ u64 reach_of(const Reach &r, int32_t entry)
 constexpr int kListThreads = 256;
 
 // Squares are added up in 64 bits: those of 32-bit gradients above 2e19 or below 1e-23 have no 32-bit value.
-template <class T> __device__ __forceinline__ double squares(const typename T::Store *p, int n)
+template <class T, int kThreads> __device__ __forceinline__ double squares(const typename T::Store *p, int n, int thread)
 {
-    constexpr int kN = Run<T>::kN, kTurn = kListThreads * kN, kAhead = 4;
+    constexpr int kN = Run<T>::kN, kTurn = kThreads * kN, kAhead = 4;
     double sum[2] = {0.0, 0.0};
-    int i = threadIdx.x * kN;
+    int i = thread * kN;
     for (; i + (kAhead - 1) * kTurn + kN <= n; i += kAhead * kTurn) {
         Run<T> r[kAhead];
 #pragma unroll
@@ -132,18 +126,17 @@ template <class T> __device__ __forceinline__ double squares(const typename T::S
 #pragma unroll
         for (int k = 0; k < kN; k++) { const double v = r.get(k); sum[k % 2] = fma(v, v, sum[k % 2]); }
     }
-    i = n / kN * kN + threadIdx.x;
+    i = n / kN * kN + thread;
     if (i < n) { const double v = (float)p[i]; sum[0] = fma(v, v, sum[0]); }
     return sum[0] + sum[1];
 }
 __global__ __launch_bounds__(kListThreads) void k_list_squares(ListView g, double *partial, uint32_t *arrived)
 {
     __shared__ double s_sum[kListThreads / kWave];
-    const Part part = part_of(g, blockIdx.x);
-    const ListEntry e = g.entry[part.entry];
+    const ListChunk c = g.chunk[blockIdx.x];
     double sum = 0.0;
-#define DGN_GO(T) sum = squares<T>(static_cast<const typename T::Store *>(e.data) + part.from, part.n)
-    DGN_BY_DTYPE(e.dtype, DGN_GO);
+#define DGN_GO(T) sum = squares<T, kListThreads>(static_cast<const typename T::Store *>(c.data), elements(c), threadIdx.x)
+    DGN_BY_DTYPE(type(c), DGN_GO);
 #undef DGN_GO
     sum = wave_sum_double(sum);
     if (lane_id() == 0) s_sum[threadIdx.x >> 6] = sum;
@@ -156,17 +149,17 @@ __global__ __launch_bounds__(kListThreads) void k_list_squares(ListView g, doubl
 
 // The chunks' sums to the sets': a lane per set, kPerGroup chunks to a workgroup, and the workgroups' sums by the one that is done last.
 // Always in the same order, so the same gradients give the same norms.
-constexpr int kPerGroup = 256;
-__global__ __launch_bounds__(kListThreads) void k_list_norms(ListView g, Reach r, const double *partial, double *sums, uint32_t *arrived, float *norms)
+constexpr int kPerGroup = 1024;
+__global__ __launch_bounds__(kPerGroup) void k_list_norms(ListView g, Reach r, const double *partial, double *sums, uint32_t *arrived, float *norms)
 {
     struct Link { double sum; u64 bits; };
     __shared__ Link s_link[kPerGroup];
-    __shared__ double s_sum[kListThreads / kWave][kWave];
+    __shared__ double s_sum[kPerGroup / kWave][kWave];
     __shared__ bool s_last;
     const int lane = lane_id(), wave = threadIdx.x >> 6;
     const int32_t chunk = blockIdx.x * kPerGroup + threadIdx.x;
     const bool some = chunk < g.chunks;
-    s_link[threadIdx.x] = Link{some ? partial[chunk] : 0.0, some ? reach_of(r, g.chunk[chunk].entry) : 0};
+    s_link[threadIdx.x] = Link{some ? partial[chunk] : 0.0, some ? reach_of(r, (int32_t)g.chunk[chunk].entry) : 0};
     __syncthreads();
     double sum = 0.0;
 #pragma unroll 4
@@ -177,7 +170,9 @@ __global__ __launch_bounds__(kListThreads) void k_list_norms(ListView g, Reach r
     s_sum[wave][lane] = sum;
     __syncthreads();
     if (wave != 0) return;
-    sum = (s_sum[0][lane] + s_sum[1][lane]) + (s_sum[2][lane] + s_sum[3][lane]);
+    sum = 0.0;
+#pragma unroll
+    for (int w = 0; w < kPerGroup / kWave; w++) sum += s_sum[w][lane];
     if (gridDim.x > 1) {
         store_coherent(reinterpret_cast<u64 *>(sums) + blockIdx.x * kWave + lane, (u64)__double_as_longlong(sum));
         __threadfence();
@@ -213,6 +208,31 @@ __device__ __forceinline__ float clip_factor(const ClipArgs &c, u64 bits, bool &
     return f;
 }
 
+// Lists of a few small tensors: all of it in one workgroup, a wave to a chunk.
+constexpr int kSmallChunks = 64, kSmallMost = 4096;
+__global__ __launch_bounds__(1024) void k_list_norms_small(ListView g, Reach r, float *norms)
+{
+    __shared__ double s_sum[16][kWave];
+    const int lane = lane_id(), wave = threadIdx.x >> 6;
+    double mine = 0.0;
+    for (int j = wave; j < g.chunks; j += 16) {
+        const ListChunk c = g.chunk[j];
+        double sum = 0.0;
+#define DGN_GO(T) sum = squares<T, kWave>(static_cast<const typename T::Store *>(c.data), elements(c), lane)
+        DGN_BY_DTYPE(type(c), DGN_GO);
+#undef DGN_GO
+        sum = wave_sum_double(sum);
+        if (reach_of(r, (int32_t)c.entry) >> lane & 1) mine += sum;
+    }
+    s_sum[wave][lane] = mine;
+    __syncthreads();
+    if (wave != 0) return;
+    mine = 0.0;
+#pragma unroll
+    for (int w = 0; w < 16; w++) mine += s_sum[w][lane];
+    if (lane < r.sets) norms[lane] = (float)sqrt(mine);
+}
+
 template <class T> __device__ __forceinline__ void scale_to(typename T::Store *out, const typename T::Store *p, int n, float f)
 {
     constexpr int kN = Run<T>::kN, kTurn = kListThreads * kN, kAhead = 4;
@@ -239,13 +259,12 @@ template <class T> __device__ __forceinline__ void scale_to(typename T::Store *o
 // The chunks from the last to the first: what the norms' pass read last is still in the cache.
 __global__ __launch_bounds__(kListThreads) void k_list_clip(ListView g, ListView out, ClipArgs cl)
 {
-    const Part part = part_of(g, gridDim.x - 1 - blockIdx.x);
-    const ListEntry e = g.entry[part.entry], o = out.entry[part.entry];
+    const ListChunk c = g.chunk[gridDim.x - 1 - blockIdx.x], o = out.chunk[gridDim.x - 1 - blockIdx.x];
     bool finite;
-    const float f = clip_factor(cl, reach_of(cl.reach, part.entry), finite);
-    if (f == 1.0f && e.data == o.data) return;
-#define DGN_GO(T) scale_to<T>(static_cast<typename T::Store *>(o.data) + part.from, static_cast<const typename T::Store *>(e.data) + part.from, part.n, f)
-    DGN_BY_DTYPE(e.dtype, DGN_GO);
+    const float f = clip_factor(cl, reach_of(cl.reach, (int32_t)c.entry), finite);
+    if (f == 1.0f && c.data == o.data) return;
+#define DGN_GO(T) scale_to<T>(static_cast<typename T::Store *>(o.data), static_cast<const typename T::Store *>(c.data), elements(c), f)
+    DGN_BY_DTYPE(type(c), DGN_GO);
 #undef DGN_GO
 }
 
@@ -296,23 +315,22 @@ __device__ __forceinline__ void adam_chunk(const AdamArgs &a, const typename T::
 }
 __global__ __launch_bounds__(kListThreads) void k_list_adam(AdamArgs a)
 {
-    const Part part = part_of(a.grad, gridDim.x - 1 - blockIdx.x);
-    const ListEntry g = a.grad.entry[part.entry];
-    const u64 bits = reach_of(a.clip.reach, part.entry);
+    const unsigned chunk = gridDim.x - 1 - blockIdx.x;
+    const ListChunk g = a.grad.chunk[chunk];
+    const u64 bits = reach_of(a.clip.reach, (int32_t)g.entry);
     bool finite = true;
     const float f = a.clip.norms ? clip_factor(a.clip, bits, finite) : 1.0f;
     const bool live = bits != 0 && (finite || !a.skip_nonfinite);
-    const auto at = [&](const ListView &l) { return static_cast<float *>(l.entry[part.entry].data) + part.from; };
+    const auto at = [&](const ListView &l) { return static_cast<float *>(l.chunk[chunk].data); };
     const AdamRow r = {at(a.param), at(a.m), at(a.v), at(a.out_param), at(a.out_m), at(a.out_v)};
     void *copy = nullptr;
     int32_t copy_type = DGN_F32;
-    if (a.copy.entries) {
-        const ListEntry c = a.copy.entry[part.entry];
-        copy_type = c.dtype;
-        copy = static_cast<char *>(c.data) + part.from * (copy_type == DGN_F32 ? 4 : 2);
+    if (a.copy.chunk) {
+        copy = a.copy.chunk[chunk].data;
+        copy_type = type(a.copy.chunk[chunk]);
     } else if (!live && r.p == r.op && r.m == r.om && r.v == r.ov) return;
-#define DGN_GO(T) adam_chunk<T>(a, static_cast<const typename T::Store *>(g.data) + part.from, r, copy, copy_type, part.n, f, live)
-    DGN_BY_DTYPE(g.dtype, DGN_GO);
+#define DGN_GO(T) adam_chunk<T>(a, static_cast<const typename T::Store *>(g.data), r, copy, copy_type, elements(g), f, live)
+    DGN_BY_DTYPE(type(g), DGN_GO);
 #undef DGN_GO
 }
 
@@ -327,9 +345,13 @@ hipError_t launch_list_norms(const ListView &g, const Reach &r, void *scratch, f
 {
     double *partial = static_cast<double *>(scratch), *sums = partial + g.chunks;
     const int groups = norm_groups(g);
+    if (g.chunks <= kSmallChunks && g.most <= kSmallMost) {
+        hipLaunchKernelGGL(k_list_norms_small, dim3(1), dim3(1024), 0, s, g, r, norms);
+        return hipGetLastError();
+    }
     uint32_t *arrived = reinterpret_cast<uint32_t *>(sums + (size_t)groups * kWave);
-    if (g.chunks > 0) hipLaunchKernelGGL(k_list_squares, dim3((unsigned)g.chunks), dim3(kListThreads), 0, s, g, partial, arrived);
-    hipLaunchKernelGGL(k_list_norms, dim3((unsigned)(groups > 0 ? groups : 1)), dim3(kListThreads), 0, s, g, r, partial, sums, arrived, norms);
+    hipLaunchKernelGGL(k_list_squares, dim3((unsigned)g.chunks), dim3(kListThreads), 0, s, g, partial, arrived);
+    hipLaunchKernelGGL(k_list_norms, dim3((unsigned)groups), dim3(kPerGroup), 0, s, g, r, partial, sums, arrived, norms);
     return hipGetLastError();
 }
 

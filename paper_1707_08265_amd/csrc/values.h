@@ -52,6 +52,7 @@ struct StepArgs {
     const float *state_in;
     float *state_out;
     void *y;
+    int64_t pieces;                 // set at the launch
 };
 bool scan_fits(int dtype, const ScanArgs &a);
 size_t scan_scratch_bytes(int dtype, const ScanArgs &a);
@@ -60,14 +61,14 @@ hipError_t launch_scan_step(int dtype, int kind, const StepArgs &a, hipStream_t 
 
 // ---- lists of tensors -----------------------------------------------------------------------------
 constexpr int kListChunk = 16384;   // elements that a workgroup takes
-struct ListEntry { void *data; int64_t numel; int32_t dtype, first_chunk; };
-struct ListChunk { int32_t entry, index; };
-struct ListView { const ListEntry *entry; const ListChunk *chunk; int32_t entries, chunks; };
+struct alignas(16) ListChunk { void *data; uint32_t entry, n_type; };    // its first element, the tensor it is of, elements * 4 + type
+static_assert(sizeof(ListChunk) == 16, "a chunk is one load");
+struct ListView { const ListChunk *chunk; int32_t chunks, most; };        // most: elements of the largest chunk
 
 struct Reach { const u64 *mask; int64_t words; const int32_t *ids; int32_t sets; };   // which sets reach an entry: see reach_of
 struct ClipArgs { Reach reach; const float *norms; float max_norm, eps; };
 struct AdamArgs {
-    ListView grad, param, m, v, out_param, out_m, out_v, copy;     // copy.entries == 0: none
+    ListView grad, param, m, v, out_param, out_m, out_v, copy;     // copy.chunk == NULL: none
     ClipArgs clip;                                                  // norms == NULL: no clipping
     float rate, beta1, rest1, beta2, rest2, eps, decay;                           // rate = lr / (1 - beta1^t), decay = lr * weight decay, rest = 1 - beta
     float spread;                                                   // 1 / (1 - beta2^t)

@@ -102,9 +102,9 @@ int check_list(const dgn_list_desc *d, int64_t *chunks)
     return DGN_OK;
 }
 
-size_t list_bytes_of(int64_t count, int64_t chunks)
+size_t list_bytes_of(int64_t chunks)
 {
-    return round256(sizeof(ListEntry) * (size_t)count) + round256(sizeof(ListChunk) * (size_t)chunks) + 256;
+    return round256(sizeof(ListChunk) * (size_t)chunks) + 256;
 }
 
 }  // namespace
@@ -196,7 +196,7 @@ int dgn_scan_step(const dgn_scan_desc *d, int64_t num_slots, const void *x, cons
         return DGN_ERR_INVALID_ARG;
     const ScanArgs s = scan_args(d);
     const StepArgs a = {s.tokens, num_slots, s.channels, s.group, s.x_stride, s.gate_stride, s.y_stride, x, gate, slots, state_in,
-                        state_out, y};
+                        state_out, y, 0};
     DGN_HIP(launch_scan_step(d->dtype, d->gate_kind, a, static_cast<hipStream_t>(stream)));
     return DGN_OK;
 }
@@ -207,7 +207,7 @@ int dgn_list_workspace(const dgn_list_desc *d, size_t *list_bytes)
     int64_t chunks = 0;
     const int rc = check_list(d, &chunks);
     if (rc != DGN_OK) return rc;
-    *list_bytes = list_bytes_of(d->count, chunks);
+    *list_bytes = list_bytes_of(chunks);
     return DGN_OK;
 }
 
@@ -218,41 +218,38 @@ int dgn_list_build(const dgn_list_desc *d, void *list_mem, size_t list_bytes, dg
     int64_t chunks = 0;
     const int rc = check_list(d, &chunks);
     if (rc != DGN_OK) return rc;
-    const size_t need = list_bytes_of(d->count, chunks);
+    const size_t need = list_bytes_of(chunks);
     if (list_bytes < need) return DGN_ERR_WORKSPACE_TOO_SMALL;
-    if (misaligned(list_mem, 8)) return DGN_ERR_INVALID_ARG;
+    if (misaligned(list_mem, 16)) return DGN_ERR_INVALID_ARG;
     dgn_list *l = new (std::nothrow) dgn_list();
     if (!l) return note_hip_error(hipErrorOutOfMemory);
-    char *host = new (std::nothrow) char[need]();
+    ListChunk *chunk = new (std::nothrow) ListChunk[need / sizeof(ListChunk)]();
     l->numel = new (std::nothrow) int64_t[d->count + 1];
     l->dtype = new (std::nothrow) int32_t[d->count + 1];
-    if (!host || !l->numel || !l->dtype) {
-        delete[] host;
+    if (!chunk || !l->numel || !l->dtype) {
+        delete[] chunk;
         dgn_list_destroy(l);
         return note_hip_error(hipErrorOutOfMemory);
     }
-    const size_t chunk_at = round256(sizeof(ListEntry) * (size_t)d->count);
-    ListEntry *entry = reinterpret_cast<ListEntry *>(host);
-    ListChunk *chunk = reinterpret_cast<ListChunk *>(host + chunk_at);
     int32_t n = 0;
     l->all_f32 = true;
     for (int64_t i = 0; i < d->count; i++) {
-        entry[i] = ListEntry{d->data[i], d->numel[i], d->dtype[i], n};
         l->numel[i] = d->numel[i];
         l->dtype[i] = d->dtype[i];
         l->all_f32 = l->all_f32 && d->dtype[i] == DGN_F32;
-        const int32_t of = (int32_t)((d->numel[i] + kListChunk - 1) / kListChunk);
-        for (int32_t j = 0; j < of; j++) chunk[n++] = ListChunk{(int32_t)i, j};
+        for (int64_t at = 0; at < d->numel[i]; at += kListChunk) {
+            const int64_t left = d->numel[i] - at, of = left < kListChunk ? left : kListChunk;
+            chunk[n++] = ListChunk{static_cast<char *>(d->data[i]) + at * element_size(d->dtype[i]), (uint32_t)i, (uint32_t)(of * 4 + d->dtype[i])};
+            if (of > l->v.most) l->v.most = (int32_t)of;
+        }
     }
     l->count = d->count;
-    l->v.entry = static_cast<const ListEntry *>(list_mem);
-    l->v.chunk = reinterpret_cast<const ListChunk *>(static_cast<char *>(list_mem) + chunk_at);
-    l->v.entries = (int32_t)d->count;
+    l->v.chunk = static_cast<const ListChunk *>(list_mem);
     l->v.chunks = n;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    hipError_t e = hipMemcpyAsync(list_mem, host, need, hipMemcpyHostToDevice, s);
+    hipError_t e = hipMemcpyAsync(list_mem, chunk, need, hipMemcpyHostToDevice, s);
     if (e == hipSuccess) e = hipStreamSynchronize(s);
-    delete[] host;
+    delete[] chunk;
     if (e != hipSuccess) {
         dgn_list_destroy(l);
         return note_hip_error(e);
