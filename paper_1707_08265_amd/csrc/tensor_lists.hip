@@ -15,6 +15,13 @@ __device__ __forceinline__ double wave_sum_double(double v)
 typedef uint32_t Quad32 __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t Quad16 __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t Pair16 __attribute__((ext_vector_type(2), aligned(2)));
+// Past the caches where kStream: see kStreamBytes.
+template <bool kStream, class V> __device__ __forceinline__ void put(V *p, V v)
+{
+    if (kStream) __builtin_nontemporal_store(v, p);
+    else *p = v;
+}
+template <bool kStream, class V> __device__ __forceinline__ V take(const V *p) { return kStream ? __builtin_nontemporal_load(p) : *p; }
 template <class T> __device__ __forceinline__ float half_of(uint32_t w, int i)
 {
     return (float)__builtin_bit_cast(typename T::Store, (uint16_t)(w >> (16 * i)));
@@ -30,7 +37,7 @@ template <> struct Run<F32> {
     static constexpr int kN = 4;
     Quad32 w;
     __device__ __forceinline__ void load(const float *p) { w = *reinterpret_cast<const Quad32 *>(p); }
-    __device__ __forceinline__ void store(float *p) const { *reinterpret_cast<Quad32 *>(p) = w; }
+    template <bool kStream> __device__ __forceinline__ void store(float *p) const { put<kStream>(reinterpret_cast<Quad32 *>(p), w); }
     __device__ __forceinline__ float get(int i) const { return __uint_as_float(w[i]); }
     __device__ __forceinline__ void scale(float f)
     {
@@ -43,7 +50,7 @@ template <class T> struct Run16 {
     static constexpr int kN = 8;
     Quad16 w;
     __device__ __forceinline__ void load(const S *p) { w = *reinterpret_cast<const Quad16 *>(p); }
-    __device__ __forceinline__ void store(S *p) const { *reinterpret_cast<Quad16 *>(p) = w; }
+    template <bool kStream> __device__ __forceinline__ void store(S *p) const { put<kStream>(reinterpret_cast<Quad16 *>(p), w); }
     __device__ __forceinline__ float get(int i) const { return half_of<T>(w[i / 2], i % 2); }
     __device__ __forceinline__ void scale(float f)
     {
@@ -56,28 +63,28 @@ template <> struct Run<BF16> : Run16<BF16> {};
 // Four elements of any type.
 template <class T> struct Four;
 template <> struct Four<F32> {
-    static __device__ __forceinline__ void load(const float *p, float (&f)[4])
+    template <bool kStream> static __device__ __forceinline__ void load(const float *p, float (&f)[4])
     {
-        const Quad32 w = *reinterpret_cast<const Quad32 *>(p);
+        const Quad32 w = take<kStream>(reinterpret_cast<const Quad32 *>(p));
 #pragma unroll
         for (int i = 0; i < 4; i++) f[i] = __uint_as_float(w[i]);
     }
-    static __device__ __forceinline__ void store(float *p, const float (&f)[4])
+    template <bool kStream> static __device__ __forceinline__ void store(float *p, const float (&f)[4])
     {
-        *reinterpret_cast<Quad32 *>(p) = Quad32{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+        put<kStream>(reinterpret_cast<Quad32 *>(p), Quad32{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])});
     }
 };
 template <class T> struct Four16 {
     typedef typename T::Store S;
-    static __device__ __forceinline__ void load(const S *p, float (&f)[4])
+    template <bool kStream> static __device__ __forceinline__ void load(const S *p, float (&f)[4])
     {
-        const Pair16 w = *reinterpret_cast<const Pair16 *>(p);
+        const Pair16 w = take<kStream>(reinterpret_cast<const Pair16 *>(p));
 #pragma unroll
         for (int i = 0; i < 4; i++) f[i] = half_of<T>(w[i / 2], i % 2);
     }
-    static __device__ __forceinline__ void store(S *p, const float (&f)[4])
+    template <bool kStream> static __device__ __forceinline__ void store(S *p, const float (&f)[4])
     {
-        *reinterpret_cast<Pair16 *>(p) = Pair16{two_halves<T>(f[0], f[1]), two_halves<T>(f[2], f[3])};
+        put<kStream>(reinterpret_cast<Pair16 *>(p), Pair16{two_halves<T>(f[0], f[1]), two_halves<T>(f[2], f[3])});
     }
 };
 template <> struct Four<F16> : Four16<F16> {};
@@ -233,7 +240,7 @@ __global__ __launch_bounds__(1024) void k_list_norms_small(ListView g, Reach r, 
     if (lane < r.sets) norms[lane] = (float)sqrt(mine);
 }
 
-template <class T> __device__ __forceinline__ void scale_to(typename T::Store *out, const typename T::Store *p, int n, float f)
+template <class T, bool kStream> __device__ __forceinline__ void scale_to(typename T::Store *out, const typename T::Store *p, int n, float f)
 {
     constexpr int kN = Run<T>::kN, kTurn = kListThreads * kN, kAhead = 4;
     int i = threadIdx.x * kN;
@@ -244,30 +251,32 @@ template <class T> __device__ __forceinline__ void scale_to(typename T::Store *o
 #pragma unroll
         for (int u = 0; u < kAhead; u++) {
             if (f != 1.0f) r[u].scale(f);
-            r[u].store(out + i + u * kTurn);
+            r[u].template store<kStream>(out + i + u * kTurn);
         }
     }
     for (; i + kN <= n; i += kTurn) {
         Run<T> r;
         r.load(p + i);
         if (f != 1.0f) r.scale(f);
-        r.store(out + i);
+        r.template store<kStream>(out + i);
     }
     i = n / kN * kN + threadIdx.x;
     if (i < n) out[i] = f != 1.0f ? (typename T::Store)((float)p[i] * f) : p[i];
 }
 // The chunks from the last to the first: what the norms' pass read last is still in the cache.
-__global__ __launch_bounds__(kListThreads) void k_list_clip(ListView g, ListView out, ClipArgs cl)
+template <bool kStream> __global__ __launch_bounds__(kListThreads) void k_list_clip(ListView g, ListView out, ClipArgs cl)
 {
     const ListChunk c = g.chunk[gridDim.x - 1 - blockIdx.x], o = out.chunk[gridDim.x - 1 - blockIdx.x];
     bool finite;
     const float f = clip_factor(cl, reach_of(cl.reach, (int32_t)c.entry), finite);
     if (f == 1.0f && c.data == o.data) return;
-#define DGN_GO(T) scale_to<T>(static_cast<typename T::Store *>(o.data), static_cast<const typename T::Store *>(c.data), elements(c), f)
+#define DGN_GO(T) scale_to<T, kStream>(static_cast<typename T::Store *>(o.data), static_cast<const typename T::Store *>(c.data), elements(c), f)
     DGN_BY_DTYPE(type(c), DGN_GO);
 #undef DGN_GO
 }
 
+// Workgroups to a chunk of the update.
+constexpr int kAdamParts = 16;
 struct AdamRow { const float *p, *m, *v; float *op, *om, *ov; };
 __device__ __forceinline__ void adam_one(const AdamArgs &a, float g, float &p, float &m, float &v)
 {
@@ -275,26 +284,26 @@ __device__ __forceinline__ void adam_one(const AdamArgs &a, float g, float &p, f
     v = a.beta2 * v + a.rest2 * (g * g);
     p -= a.decay * p + a.rate * m / (sqrtf(v * a.spread) + a.eps);
 }
-template <class T>
+template <class T, bool kStream>
 __device__ __forceinline__ void adam_chunk(const AdamArgs &a, const typename T::Store *g, const AdamRow &r, void *copy, int32_t copy_type, int n,
                                            float f, bool live)
 {
     constexpr int kTurn = kListThreads * 4;
     for (int i = threadIdx.x * 4; i + 4 <= n; i += kTurn) {
         float d[4], p[4], m[4], v[4];
-        Four<T>::load(g + i, d);
-        Four<F32>::load(r.p + i, p);
-        Four<F32>::load(r.m + i, m);
-        Four<F32>::load(r.v + i, v);
+        Four<T>::template load<kStream>(g + i, d);
+        Four<F32>::load<kStream>(r.p + i, p);
+        Four<F32>::load<kStream>(r.m + i, m);
+        Four<F32>::load<kStream>(r.v + i, v);
         if (live) {
 #pragma unroll
             for (int k = 0; k < 4; k++) adam_one(a, d[k] * f, p[k], m[k], v[k]);
         }
-        Four<F32>::store(r.op + i, p);
-        Four<F32>::store(r.om + i, m);
-        Four<F32>::store(r.ov + i, v);
+        Four<F32>::store<kStream>(r.op + i, p);
+        Four<F32>::store<kStream>(r.om + i, m);
+        Four<F32>::store<kStream>(r.ov + i, v);
         if (copy) {
-#define DGN_GO(C) Four<C>::store(static_cast<typename C::Store *>(copy) + i, p)
+#define DGN_GO(C) Four<C>::template store<kStream>(static_cast<typename C::Store *>(copy) + i, p)
             DGN_BY_DTYPE(copy_type, DGN_GO);
 #undef DGN_GO
         }
@@ -313,23 +322,27 @@ __device__ __forceinline__ void adam_chunk(const AdamArgs &a, const typename T::
         }
     }
 }
-__global__ __launch_bounds__(kListThreads) void k_list_adam(AdamArgs a)
+template <bool kStream> __global__ __launch_bounds__(kListThreads) void k_list_adam(AdamArgs a)
 {
-    const unsigned chunk = gridDim.x - 1 - blockIdx.x;
+    const unsigned number = gridDim.x - 1 - blockIdx.x, chunk = number / kAdamParts;
     const ListChunk g = a.grad.chunk[chunk];
+    const int first = (int)(number % kAdamParts) * (kListChunk / kAdamParts), left = elements(g) - first;
+    const int n = left < kListChunk / kAdamParts ? left : kListChunk / kAdamParts;
+    if (n <= 0) return;
     const u64 bits = reach_of(a.clip.reach, (int32_t)g.entry);
     bool finite = true;
     const float f = a.clip.norms ? clip_factor(a.clip, bits, finite) : 1.0f;
     const bool live = bits != 0 && (finite || !a.skip_nonfinite);
-    const auto at = [&](const ListView &l) { return static_cast<float *>(l.chunk[chunk].data); };
+    const auto at = [&](const ListView &l) { return static_cast<float *>(l.chunk[chunk].data) + first; };
     const AdamRow r = {at(a.param), at(a.m), at(a.v), at(a.out_param), at(a.out_m), at(a.out_v)};
     void *copy = nullptr;
     int32_t copy_type = DGN_F32;
     if (a.copy.chunk) {
-        copy = a.copy.chunk[chunk].data;
-        copy_type = type(a.copy.chunk[chunk]);
+        const ListChunk c = a.copy.chunk[chunk];
+        copy_type = type(c);
+        copy = static_cast<char *>(c.data) + first * (copy_type == DGN_F32 ? 4 : 2);
     } else if (!live && r.p == r.op && r.m == r.om && r.v == r.ov) return;
-#define DGN_GO(T) adam_chunk<T>(a, static_cast<const typename T::Store *>(g.data), r, copy, copy_type, elements(g), f, live)
+#define DGN_GO(T) adam_chunk<T, kStream>(a, static_cast<const typename T::Store *>(g.data) + first, r, copy, copy_type, n, f, live)
     DGN_BY_DTYPE(type(g), DGN_GO);
 #undef DGN_GO
 }
@@ -357,13 +370,18 @@ hipError_t launch_list_norms(const ListView &g, const Reach &r, void *scratch, f
 
 hipError_t launch_list_clip(const ListView &g, const ListView &out, const ClipArgs &c, hipStream_t s)
 {
-    if (g.chunks > 0) hipLaunchKernelGGL(k_list_clip, dim3((unsigned)g.chunks), dim3(kListThreads), 0, s, g, out, c);
+    if (g.chunks == 0) return hipSuccess;
+    if (g.bytes + out.bytes > kStreamBytes) hipLaunchKernelGGL(k_list_clip<true>, dim3((unsigned)g.chunks), dim3(kListThreads), 0, s, g, out, c);
+    else hipLaunchKernelGGL(k_list_clip<false>, dim3((unsigned)g.chunks), dim3(kListThreads), 0, s, g, out, c);
     return hipGetLastError();
 }
 
 hipError_t launch_list_adam(const AdamArgs &a, hipStream_t s)
 {
-    if (a.grad.chunks > 0) hipLaunchKernelGGL(k_list_adam, dim3((unsigned)a.grad.chunks), dim3(kListThreads), 0, s, a);
+    if (a.grad.chunks == 0) return hipSuccess;
+    const size_t bytes = a.grad.bytes + 6 * a.param.bytes + a.copy.bytes;
+    if (bytes > kStreamBytes) hipLaunchKernelGGL(k_list_adam<true>, dim3((unsigned)a.grad.chunks * kAdamParts), dim3(kListThreads), 0, s, a);
+    else hipLaunchKernelGGL(k_list_adam<false>, dim3((unsigned)a.grad.chunks * kAdamParts), dim3(kListThreads), 0, s, a);
     return hipGetLastError();
 }
 

@@ -94,7 +94,7 @@ int check_list(const dgn_list_desc *d, int64_t *chunks)
         if (d->numel[i] < 0 || !type_known(d->dtype[i])) return DGN_ERR_INVALID_ARG;
         if (d->numel[i] > ((int64_t)1 << 44)) return DGN_ERR_TOO_LARGE;
         n += (d->numel[i] + kListChunk - 1) / kListChunk;
-        if (n > kMaxCount / 256) return DGN_ERR_TOO_LARGE;      // a launch holds less than 2^32 threads
+        if (n > kMaxCount / 1024) return DGN_ERR_TOO_LARGE;      // a launch holds less than 2^32 threads
         if (d->numel[i] > 0 && !d->data[i]) return DGN_ERR_NULL_PTR;
         if (misaligned(d->data[i], element_size(d->dtype[i]))) return DGN_ERR_INVALID_ARG;
     }
@@ -235,6 +235,7 @@ int dgn_list_build(const dgn_list_desc *d, void *list_mem, size_t list_bytes, dg
     l->all_f32 = true;
     for (int64_t i = 0; i < d->count; i++) {
         l->numel[i] = d->numel[i];
+        l->v.bytes += (size_t)d->numel[i] * element_size(d->dtype[i]);
         l->dtype[i] = d->dtype[i];
         l->all_f32 = l->all_f32 && d->dtype[i] == DGN_F32;
         for (int64_t at = 0; at < d->numel[i]; at += kListChunk) {
