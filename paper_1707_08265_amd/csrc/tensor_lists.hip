@@ -109,12 +109,13 @@ __device__ __forceinline__ u64 reach_of(const Reach &r, int32_t entry)
     return at >= 0 && at < r.words ? r.mask[at] & all : 0;
 }
 
-constexpr int kListThreads = 256;
+constexpr int kListThreads = 256, kClipParts = 2;      // (parts: workgroups to a chunk)
+constexpr int kAdamThreads = 512, kAdamParts = 4;
 
 // Squares are added up in 64 bits: those of 32-bit gradients above 2e19 or below 1e-23 have no 32-bit value.
 template <class T, int kThreads> __device__ __forceinline__ double squares(const typename T::Store *p, int n, int thread)
 {
-    constexpr int kN = Run<T>::kN, kTurn = kThreads * kN, kAhead = 4;
+    constexpr int kN = Run<T>::kN, kTurn = kThreads * kN, kAhead = 2;
     double sum[2] = {0.0, 0.0};
     int i = thread * kN;
     for (; i + (kAhead - 1) * kTurn + kN <= n; i += kAhead * kTurn) {
@@ -242,7 +243,7 @@ __global__ __launch_bounds__(1024) void k_list_norms_small(ListView g, Reach r, 
 
 template <class T, bool kStream> __device__ __forceinline__ void scale_to(typename T::Store *out, const typename T::Store *p, int n, float f)
 {
-    constexpr int kN = Run<T>::kN, kTurn = kListThreads * kN, kAhead = 4;
+    constexpr int kN = Run<T>::kN, kTurn = kListThreads * kN, kAhead = 2;
     int i = threadIdx.x * kN;
     for (; i + (kAhead - 1) * kTurn + kN <= n; i += kAhead * kTurn) {
         Run<T> r[kAhead];
@@ -266,17 +267,19 @@ template <class T, bool kStream> __device__ __forceinline__ void scale_to(typena
 // The chunks from the last to the first: what the norms' pass read last is still in the cache.
 template <bool kStream> __global__ __launch_bounds__(kListThreads) void k_list_clip(ListView g, ListView out, ClipArgs cl)
 {
-    const ListChunk c = g.chunk[gridDim.x - 1 - blockIdx.x], o = out.chunk[gridDim.x - 1 - blockIdx.x];
+    const unsigned number = gridDim.x - 1 - blockIdx.x, chunk = number / kClipParts;
+    const ListChunk c = g.chunk[chunk], o = out.chunk[chunk];
+    const int first = (int)(number % kClipParts) * (kListChunk / kClipParts), left = elements(c) - first;
+    const int n = left < kListChunk / kClipParts ? left : kListChunk / kClipParts;
+    if (n <= 0) return;
     bool finite;
     const float f = clip_factor(cl, reach_of(cl.reach, (int32_t)c.entry), finite);
     if (f == 1.0f && c.data == o.data) return;
-#define DGN_GO(T) scale_to<T, kStream>(static_cast<typename T::Store *>(o.data), static_cast<const typename T::Store *>(c.data), elements(c), f)
+#define DGN_GO(T) scale_to<T, kStream>(static_cast<typename T::Store *>(o.data) + first, static_cast<const typename T::Store *>(c.data) + first, n, f)
     DGN_BY_DTYPE(type(c), DGN_GO);
 #undef DGN_GO
 }
 
-// Workgroups to a chunk of the update.
-constexpr int kAdamParts = 16;
 struct AdamRow { const float *p, *m, *v; float *op, *om, *ov; };
 __device__ __forceinline__ void adam_one(const AdamArgs &a, float g, float &p, float &m, float &v)
 {
@@ -288,7 +291,7 @@ template <class T, bool kStream>
 __device__ __forceinline__ void adam_chunk(const AdamArgs &a, const typename T::Store *g, const AdamRow &r, void *copy, int32_t copy_type, int n,
                                            float f, bool live)
 {
-    constexpr int kTurn = kListThreads * 4;
+    constexpr int kTurn = kAdamThreads * 4;
     for (int i = threadIdx.x * 4; i + 4 <= n; i += kTurn) {
         float d[4], p[4], m[4], v[4];
         Four<T>::template load<kStream>(g + i, d);
@@ -322,11 +325,11 @@ __device__ __forceinline__ void adam_chunk(const AdamArgs &a, const typename T::
         }
     }
 }
-template <bool kStream> __global__ __launch_bounds__(kListThreads) void k_list_adam(AdamArgs a)
+template <bool kStream> __global__ __launch_bounds__(kAdamThreads) void k_list_adam(AdamArgs a)
 {
-    const unsigned number = gridDim.x - 1 - blockIdx.x, chunk = number / kAdamParts;
+    const unsigned chunk = blockIdx.x / kAdamParts;
     const ListChunk g = a.grad.chunk[chunk];
-    const int first = (int)(number % kAdamParts) * (kListChunk / kAdamParts), left = elements(g) - first;
+    const int first = (int)(blockIdx.x % kAdamParts) * (kListChunk / kAdamParts), left = elements(g) - first;
     const int n = left < kListChunk / kAdamParts ? left : kListChunk / kAdamParts;
     if (n <= 0) return;
     const u64 bits = reach_of(a.clip.reach, (int32_t)g.entry);
@@ -371,8 +374,8 @@ hipError_t launch_list_norms(const ListView &g, const Reach &r, void *scratch, f
 hipError_t launch_list_clip(const ListView &g, const ListView &out, const ClipArgs &c, hipStream_t s)
 {
     if (g.chunks == 0) return hipSuccess;
-    if (g.bytes + out.bytes > kStreamBytes) hipLaunchKernelGGL(k_list_clip<true>, dim3((unsigned)g.chunks), dim3(kListThreads), 0, s, g, out, c);
-    else hipLaunchKernelGGL(k_list_clip<false>, dim3((unsigned)g.chunks), dim3(kListThreads), 0, s, g, out, c);
+    if (g.bytes + out.bytes > kStreamBytes) hipLaunchKernelGGL(k_list_clip<true>, dim3((unsigned)g.chunks * kClipParts), dim3(kListThreads), 0, s, g, out, c);
+    else hipLaunchKernelGGL(k_list_clip<false>, dim3((unsigned)g.chunks * kClipParts), dim3(kListThreads), 0, s, g, out, c);
     return hipGetLastError();
 }
 
@@ -380,8 +383,8 @@ hipError_t launch_list_adam(const AdamArgs &a, hipStream_t s)
 {
     if (a.grad.chunks == 0) return hipSuccess;
     const size_t bytes = a.grad.bytes + 6 * a.param.bytes + a.copy.bytes;
-    if (bytes > kStreamBytes) hipLaunchKernelGGL(k_list_adam<true>, dim3((unsigned)a.grad.chunks * kAdamParts), dim3(kListThreads), 0, s, a);
-    else hipLaunchKernelGGL(k_list_adam<false>, dim3((unsigned)a.grad.chunks * kAdamParts), dim3(kListThreads), 0, s, a);
+    if (bytes > kStreamBytes) hipLaunchKernelGGL(k_list_adam<true>, dim3((unsigned)a.grad.chunks * kAdamParts), dim3(kAdamThreads), 0, s, a);
+    else hipLaunchKernelGGL(k_list_adam<false>, dim3((unsigned)a.grad.chunks * kAdamParts), dim3(kAdamThreads), 0, s, a);
     return hipGetLastError();
 }
 

@@ -60,7 +60,7 @@ hipError_t launch_scan(int dtype, int kind, bool back, const ScanArgs &a, void *
 hipError_t launch_scan_step(int dtype, int kind, const StepArgs &a, hipStream_t s);
 
 // ---- lists of tensors -----------------------------------------------------------------------------
-constexpr int kListChunk = 16384;   // elements that a workgroup takes
+constexpr int kListChunk = 8192;    // elements of a chunk
 struct alignas(16) ListChunk { void *data; uint32_t entry, n_type; };    // its first element, the tensor it is of, elements * 4 + type
 static_assert(sizeof(ListChunk) == 16, "a chunk is one load");
 struct ListView { const ListChunk *chunk; int32_t chunks, most; size_t bytes; };      // most: elements of the largest chunk; bytes: of all
