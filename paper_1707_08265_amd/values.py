@@ -127,11 +127,12 @@ class TensorList:
         n = len(self.tensors)
         dev = self.tensors[0].device if n else torch.device("cuda", torch.cuda.current_device())
         for t in self.tensors:
-            _need(isinstance(t, torch.Tensor) and t.dtype in DTYPES and t.device == dev and t.is_contiguous(), "TensorList")
+            if not (isinstance(t, torch.Tensor) and t.dtype in DTYPES and t.is_contiguous() and t.device == dev):
+                raise b.DgnError(b.DGN_ERR_INVALID_ARG, "TensorList")
         self.device = dev
-        self._numel = np.array([t.numel() for t in self.tensors] or [0], dtype=np.int64)
-        data = np.array([t.data_ptr() for t in self.tensors] or [0], dtype=np.uint64)
-        types = np.array([DTYPES[t.dtype] for t in self.tensors] or [0], dtype=np.int32)
+        self._numel = np.fromiter((t.numel() for t in self.tensors), np.int64, n)
+        data = np.fromiter((t.data_ptr() for t in self.tensors), np.uint64, n)
+        types = np.fromiter((DTYPES[t.dtype] for t in self.tensors), np.int32, n)
         desc = b.dgn_list_desc(count=n, data=data.ctypes.data, numel=self._numel.ctypes.data, dtype=types.ctypes.data)
         self.handle = None
         rc, nb = b.dgn_list_workspace(desc)
