@@ -56,12 +56,12 @@ template <class T, int V> struct Pack {
             for (int i = 0; i < 4; i++) w[i % kWords] = v[i];
         }
     }
-    __device__ __forceinline__ void store(S *p) const
+    template <bool kStream = false> __device__ __forceinline__ void store(S *p) const
     {
-        if (kBytes == 2) *reinterpret_cast<uint16_t *>(p) = (uint16_t)w[0];
-        else if (kBytes == 4) *reinterpret_cast<Word *>(p) = w[0];
-        else if (kBytes == 8) *reinterpret_cast<Pair *>(p) = Pair{w[0], w[1 % kWords]};
-        else *reinterpret_cast<Quad4 *>(p) = Quad4{w[0], w[1 % kWords], w[2 % kWords], w[3 % kWords]};
+        if (kBytes == 2) put<kStream>(reinterpret_cast<uint16_t *>(p), (uint16_t)w[0]);
+        else if (kBytes == 4) put<kStream>(reinterpret_cast<Word *>(p), (Word)w[0]);
+        else if (kBytes == 8) put<kStream>(reinterpret_cast<Pair *>(p), Pair{w[0], w[1 % kWords]});
+        else put<kStream>(reinterpret_cast<Quad4 *>(p), Quad4{w[0], w[1 % kWords], w[2 % kWords], w[3 % kWords]});
     }
     __device__ __forceinline__ float get(int i) const
     {
@@ -402,7 +402,7 @@ template <int V> __device__ __forceinline__ void state_before(const ScanArgs &a,
 }
 
 // Third launch, forward.  The strips from the last to the first: what the first launch read last is still in the cache.
-template <class T, int kKind, int V, bool kShared>
+template <class T, int kKind, int V, bool kShared, bool kStream>
 __global__ __launch_bounds__(kStripWaves *kWave, 8) void k_scan_outputs(ScanArgs a)
 {
     typedef typename T::Store S;
@@ -441,7 +441,7 @@ __global__ __launch_bounds__(kStripWaves *kWave, 8) void k_scan_outputs(ScanArgs
             if (k0 + k >= st.from && k0 + k < st.to) {
                 Pack<T, V> out;
                 out.set(h);
-                out.store(y + st.mine);
+                out.template store<kStream>(y + st.mine);
             }
             y += a.y_stride;
             if ((end.bits >> k & 1) && a.final) store_state<V>(row_of(a.final, __builtin_amdgcn_readlane(end.id, k), a, st.c), st.mine, h);
@@ -471,7 +471,7 @@ template <int kTokens> __device__ __forceinline__ void sum_heads(float (&v)[kTok
 }
 
 // Third launch, backward.  kKeep rows at a time, the last first: the states before each of them from the one that is kept, then the gradients.
-template <class T, int kKind, int V, bool kShared>
+template <class T, int kKind, int V, bool kShared, bool kStream>
 __global__ __launch_bounds__(kStripWaves *kWave, 4) void k_scan_gradients(ScanArgs a)
 {
     typedef typename T::Store S;
@@ -537,10 +537,10 @@ __global__ __launch_bounds__(kStripWaves *kWave, 4) void k_scan_gradients(ScanAr
                 if (k0 + k >= st.from && k0 + k < st.to) {
                     Pack<T, V> out;
                     out.set(dx);
-                    out.store(px + st.mine);
+                    out.template store<kStream>(px + st.mine);
                     if (!kShared) {
                         out.set(dg);
-                        out.store(pg + st.mine);
+                        out.template store<kStream>(pg + st.mine);
                     }
                 }
                 if ((begin.bits >> k & 1) && a.dh0) store_state<V>(row_of(a.dh0, __builtin_amdgcn_readlane(begin.id, k), a, st.c), st.mine, e);
@@ -666,13 +666,18 @@ template <class T, int kKind, int V, bool kShared> static void go_forward(const 
 {
     if (a.strips > 1) hipLaunchKernelGGL((k_scan_links<T, kKind, V, kShared, false>), grid_of(a), dim3(kStripWaves * kWave), 0, s, a);
     if (a.states) scan_states(a, V, false, s);
-    hipLaunchKernelGGL((k_scan_outputs<T, kKind, V, kShared>), grid_of(a), dim3(kStripWaves * kWave), 0, s, a);
+    // x, gate and y; x, gate, dy, dx and dgate (of the backward pass)
+    if (a.tokens * (2 * a.channels + a.heads) * sizeof(typename T::Store) > kStreamBytes)
+        hipLaunchKernelGGL((k_scan_outputs<T, kKind, V, kShared, true>), grid_of(a), dim3(kStripWaves * kWave), 0, s, a);
+    else hipLaunchKernelGGL((k_scan_outputs<T, kKind, V, kShared, false>), grid_of(a), dim3(kStripWaves * kWave), 0, s, a);
 }
 template <class T, int kKind, int V, bool kShared> static void go_backward(const ScanArgs &a, hipStream_t s)
 {
     if (a.strips > 1) hipLaunchKernelGGL((k_scan_links<T, kKind, V, kShared, true>), grid_of(a), dim3(kStripWaves * kWave), 0, s, a);
     if (a.states) scan_states(a, V, true, s);
-    hipLaunchKernelGGL((k_scan_gradients<T, kKind, V, kShared>), grid_of(a), dim3(kStripWaves * kWave), 0, s, a);
+    if (a.tokens * (3 * a.channels + 2 * a.heads) * sizeof(typename T::Store) > kStreamBytes)
+        hipLaunchKernelGGL((k_scan_gradients<T, kKind, V, kShared, true>), grid_of(a), dim3(kStripWaves * kWave), 0, s, a);
+    else hipLaunchKernelGGL((k_scan_gradients<T, kKind, V, kShared, false>), grid_of(a), dim3(kStripWaves * kWave), 0, s, a);
     if (a.parts > 1 && a.tokens > 0) {
         const int64_t n = (a.tokens * a.heads + 255) / 256;
         hipLaunchKernelGGL((k_gate_sums<T>), dim3((unsigned)(n < 8192 ? n : 8192)), dim3(256), 0, s, a);

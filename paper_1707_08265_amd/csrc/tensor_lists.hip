@@ -15,13 +15,6 @@ __device__ __forceinline__ double wave_sum_double(double v)
 typedef uint32_t Quad32 __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t Quad16 __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t Pair16 __attribute__((ext_vector_type(2), aligned(2)));
-// Past the caches where kStream: see kStreamBytes.
-template <bool kStream, class V> __device__ __forceinline__ void put(V *p, V v)
-{
-    if (kStream) __builtin_nontemporal_store(v, p);
-    else *p = v;
-}
-template <bool kStream, class V> __device__ __forceinline__ V take(const V *p) { return kStream ? __builtin_nontemporal_load(p) : *p; }
 template <class T> __device__ __forceinline__ float half_of(uint32_t w, int i)
 {
     return (float)__builtin_bit_cast(typename T::Store, (uint16_t)(w >> (16 * i)));

@@ -15,6 +15,13 @@ struct BF16 { typedef __bf16 Store; };
 
 inline int element_size(int32_t dtype) { return dtype == DGN_F32 ? 4 : 2; }
 
+// Past the caches where kStream (see kStreamBytes).
+template <bool kStream, class V> __device__ __forceinline__ V take(const V *p) { return kStream ? __builtin_nontemporal_load(p) : *p; }
+template <bool kStream, class V> __device__ __forceinline__ void put(V *p, V v)
+{
+    if (kStream) __builtin_nontemporal_store(v, p);
+    else *p = v;
+}
 // What lanes of a wave wrote to LDS is there for the others.
 __device__ __forceinline__ void wave_fence()
 {
