@@ -141,7 +141,7 @@ __device__ __forceinline__ Block block_of(const ScanArgs &a, int64_t block)
 
 
 constexpr int kKeep = kScanKeep;        // rows between two states that the forward pass keeps for the backward pass
-constexpr int kMostRows = 128;          // rows of a strip, at most
+constexpr int kMostRows = 64;           // rows of a strip, at most
 constexpr int kStripWaves = 4;          // waves of a workgroup; each has a strip of its own
 
 // Where sequences begin and end in the rows of a strip, a wave's own.
@@ -184,7 +184,7 @@ __device__ __forceinline__ float *row_of(float *p, int32_t row, const ScanArgs &
 template <int V, bool kShared> struct Strip {
     int64_t row0, c, head0;     // first row, first channel, and the head that has it
     int32_t rows, from, to;     // rows of it; those from `from` on, before `to`, belong to sequences
-    int32_t part;
+    int32_t part, width;        // which part of a head, and the channels of the block
     int64_t strip, number;      // and the number of the block
     uint32_t mine, head;        // the lane's place in the block, and its head's (32 bits: what is the same for the wave stays in scalar registers)
     bool active, last, marked, empties;
@@ -200,6 +200,7 @@ template <int V, bool kShared> struct Strip {
         number = strip_block;
         c = bl.c;
         part = bl.part;
+        width = bl.width;
         active = lane_id() * V < bl.width;
         mine = active ? lane_id() * V : 0;
         head = kShared ? mine / (uint32_t)a.group : 0;
@@ -354,8 +355,11 @@ __global__ __launch_bounds__(kStripWaves *kWave, 8) void k_scan_links(ScanArgs a
 }
 
 // Second launch: the state that comes into each strip, states[strip][slot].  A workgroup has kSlots slots; the strips are cut into kPieces
-// pieces, each is put together, the pieces' links are applied one after the other, and each is gone through again.
+// pieces, each is put together, the pieces' links are applied one after the other, and each is gone through again: with its words in
+// registers where they are few (kEach > 0: at most so many), so that they are asked for once and all at once: 625 strips of 1 024 slots 6.5
+// instead of 8.3 us.  (With 32 of them, for 1 025 strips, 16.7 us instead of 10.2: too many registers for 1 024 threads.)
 constexpr int kSlots = 16, kPieces = 64;
+template <int kEach>
 __global__ __launch_bounds__(kSlots *kPieces) void k_scan_states(const u64 *words, float *states, int64_t strips, int64_t slots, bool back)
 {
     __shared__ u64 s_link[kPieces][kSlots];
@@ -363,20 +367,36 @@ __global__ __launch_bounds__(kSlots *kPieces) void k_scan_states(const u64 *word
     const int piece = threadIdx.x / kSlots;
     const int64_t each = (strips + kPieces - 1) / kPieces, from = piece * each, to = from + each < strips ? from + each : strips;
     const auto row = [&](int64_t n) { return (back ? strips - 1 - n : n) * slots + slot; };
+    u64 kept[kEach > 0 ? kEach : 1];
     float A = 1.0f, B = 0.0f;
     bool cut = false;
-#pragma unroll 8
-    for (int64_t n = from; n < to; n++) {
-        const u64 w = words[row(n)];
+    const auto join = [&](u64 w) {
         B = apply_word(w, B);
         A *= __uint_as_float((uint32_t)(w >> 32));
         cut = cut || word_cuts(w);
+    };
+    if (kEach > 0) {
+#pragma unroll
+        for (int k = 0; k < kEach; k++) kept[k] = from + k < to ? words[row(from + k)] : link_word(1.0f, 0.0f, false);
+#pragma unroll
+        for (int k = 0; k < kEach; k++) join(kept[k]);
+    } else {
+#pragma unroll 8
+        for (int64_t n = from; n < to; n++) join(words[row(n)]);
     }
     s_link[piece][threadIdx.x % kSlots] = link_word(A, B, cut);
     __syncthreads();
     float h = 0.0f;
 #pragma unroll 8
     for (int p = 0; p < piece; p++) h = apply_word(s_link[p][threadIdx.x % kSlots], h);
+    if (kEach > 0) {
+#pragma unroll
+        for (int k = 0; k < kEach; k++) {
+            if (from + k < to) states[row(from + k)] = h;
+            h = apply_word(kept[k], h);
+        }
+        return;
+    }
 #pragma unroll 8
     for (int64_t n = from; n < to; n++) {
         const u64 w = words[row(n)];
@@ -449,25 +469,39 @@ __global__ __launch_bounds__(kStripWaves *kWave, 8) void k_scan_outputs(ScanArgs
     }
 }
 
-// Sums of kTokens values a lane over the lanes of each head (`lanes` of them, the first head's from lane 0 on); the result for token k of
-// a head is in v[k] of its first lane.
-template <int kTokens> __device__ __forceinline__ void sum_heads(float (&v)[kTokens], int lanes, int lane)
+// Sums of N values a lane (of rows `row` ...) over groups of 2 d lanes, handed to write(row, sum) by one lane of each.  At each step two lanes
+// share out the values that are left: 17 exchanges for 16 values over 64 lanes, not 96.
+template <int N, class F> __device__ __forceinline__ void sum_lanes(const float (&v)[N], int d, int row, bool writes, F write)
 {
-    if ((lanes & (lanes - 1)) == 0) {
-        for (int d = lanes >> 1; d >= 1; d >>= 1) {
+    if (d == 0) {
 #pragma unroll
-            for (int k = 0; k < kTokens; k++) v[k] += __shfl_xor(v[k], d, kWave);
-        }
+        for (int k = 0; k < N; k++) if (writes) write(row + k, v[k]);
         return;
     }
-    const int at = lane % lanes;
+    const bool upper = lane_id() & d;
+    if constexpr (N == 1) {
+        const float both[1] = {v[0] + __shfl_xor(v[0], d, kWave)};
+        sum_lanes<1>(both, d >> 1, row, writes && !upper, write);
+    } else {
+        float half[N / 2];
+#pragma unroll
+        for (int k = 0; k < N / 2; k++) half[k] = (upper ? v[k + N / 2] : v[k]) + __shfl_xor(upper ? v[k] : v[k + N / 2], d, kWave);
+        sum_lanes<N / 2>(half, d >> 1, upper ? row + N / 2 : row, writes, write);
+    }
+}
+// The same over groups of any number of lanes, the first from lane 0 on.
+template <int N, class F> __device__ __forceinline__ void sum_any_lanes(float (&v)[N], int lanes, bool writes, F write)
+{
+    const int at = lane_id() % lanes;
     for (int d = 1; d < lanes; d <<= 1) {
 #pragma unroll
-        for (int k = 0; k < kTokens; k++) {
+        for (int k = 0; k < N; k++) {
             const float o = __shfl_down(v[k], d, kWave);
-            if (at + d < lanes && lane + d < kWave) v[k] += o;
+            if (at + d < lanes && lane_id() + d < kWave) v[k] += o;
         }
     }
+#pragma unroll
+    for (int k = 0; k < N; k++) if (writes && at == 0) write(k, v[k]);
 }
 
 // Third launch, backward.  kKeep rows at a time, the last first: the states before each of them from the one that is kept, then the gradients.
@@ -478,6 +512,7 @@ __global__ __launch_bounds__(kStripWaves *kWave, 4) void k_scan_gradients(ScanAr
     constexpr int kTokens = kKeep;
     __shared__ Marks s_marks[kStripWaves];
     Marks &marks = s_marks[wave_id()];
+    __shared__ float s_sums[kShared ? kStripWaves : 1][kShared ? kTokens * kWave : 1];
     Strip<V, kShared> st;
     if (!st.find(a, (int64_t)blockIdx.x * kStripWaves + wave_id(), true)) return;
     float e[V];
@@ -549,21 +584,27 @@ __global__ __launch_bounds__(kStripWaves *kWave, 4) void k_scan_gradients(ScanAr
             pg -= a.dgate_stride;
         }
         if (kShared) {
-            // (a part of a head is all lanes of its block; the lanes past its end count nothing)
+            // (a part of a head is all lanes of its block, and has one place; the lanes past its end count nothing)
             if (!st.active) {
 #pragma unroll
                 for (int k = 0; k < kTokens; k++) sum[k] = 0.0f;
             }
             const int lanes = a.parts > 1 ? kWave : (int)(a.group / V);
-            sum_heads(sum, lanes, lane_id());
-            if (st.active && lane_id() % lanes == 0) {
-#pragma unroll
-                for (int k = 0; k < kTokens; k++) {
-                    if (k0 + k < st.from || k0 + k >= st.to) continue;
-                    if (a.parts > 1) a.partial[(st.part * a.tokens + row0 + k) * a.heads + st.head0 + st.head] = sum[k];
-                    else static_cast<S *>(a.dgate)[(row0 + k) * a.dgate_stride + st.head0 + st.head] = (S)sum[k];
-                }
+            float *sums = s_sums[wave_id()];            // [row][head of the block]
+            const auto write = [&](int k, float v) { sums[k * kWave + st.head] = v; };
+            const bool writes = st.active || a.parts > 1;
+            if ((lanes & (lanes - 1)) == 0) sum_lanes<kTokens>(sum, lanes >> 1, 0, writes, write);
+            else sum_any_lanes<kTokens>(sum, lanes, writes, write);
+            wave_fence();
+            const int heads = a.parts > 1 ? 1 : (int)(st.width / (int32_t)a.group);
+            for (int i = lane_id(); i < kTokens * heads; i += kWave) {
+                const int k = i / heads, head = i - k * heads;
+                if (k0 + k < st.from || k0 + k >= st.to) continue;
+                const float v = sums[k * kWave + head];
+                if (a.parts > 1) a.partial[(st.part * a.tokens + row0 + k) * a.heads + st.head0] = v;
+                else static_cast<S *>(a.dgate)[(row0 + k) * a.dgate_stride + st.head0 + head] = (S)v;
             }
+            wave_fence();
         }
     }
 }
@@ -614,53 +655,50 @@ __global__ __launch_bounds__(256) void k_scan_step(StepArgs a)
     }
 }
 
-// Elements a thread takes of a row, as the rows' and the heads' numbers allow: forward eight bytes, where there are channels enough for a
-// wave of them, else four; backward, with three rows to keep, four.
-static int elements_of(int dtype, const ScanArgs &a, bool back)
+// Elements a thread takes of a row: four bytes of them, as the rows' and the heads' numbers allow.  (Eight bytes forward: 10 000 x 1 000
+// 32.5 instead of 30.6 us, 257 x 512 14.6 instead of 12.2, with half as many waves to ask for rows.)
+static int elements_of(int dtype, const ScanArgs &a)
 {
     const int64_t unit = a.group == 1 ? a.channels : a.group;      // (heads that are cut into parts are cut at multiples of V)
-    const int words = back || a.channels <= (dtype == DGN_F32 ? 64 : 128) ? 1 : 2, most = words * (dtype == DGN_F32 ? 1 : 2);
-    return unit % 4 == 0 ? most : unit % 2 == 0 && most > 2 ? 2 : unit % 2 == 0 ? most : 1;
+    return dtype != DGN_F32 && unit % 2 == 0 ? 2 : 1;
 }
 
-// Strips: as many as fill the waves of the card several times over (kStrips of them), of kKeep to kMostRows rows.
-constexpr int64_t kStrips = 8192;
-constexpr int64_t kFewStrips = 32;      // up to here a strip applies the links before it itself: 257 x 512 forward 14.9 us instead of 16.6
+// Rows of a strip: as few as give kStrips strips, which is what the card has waves for, and at least so many that a channel has no
+// more strips than the second launch keeps in registers -- from kKeep to kMostRows.
+constexpr int64_t kStrips = 8192, kChannelStrips = 1024;
+constexpr int64_t kFewStrips = 32;      // up to here a strip applies the links before it itself: 257 x 512 forward 14.6 us instead of 16.6
 struct Layout { int V; Cut cut; int64_t rows, strips; size_t words, states, partial, bytes; };
-static Layout lay_out(int dtype, const ScanArgs &a, bool back)
+static Layout lay_out(int dtype, const ScanArgs &a)
 {
     Layout l;
-    l.V = elements_of(dtype, a, back);
+    l.V = elements_of(dtype, a);
     l.cut = cut_channels(a.channels, a.group, l.V);
-    const int64_t want = a.tokens * l.cut.blocks / kStrips;
-    l.rows = want < kKeep ? kKeep : want > kMostRows ? kMostRows : want / kKeep * kKeep;
+    const int64_t want = a.tokens * l.cut.blocks / kStrips, least = (a.tokens + kChannelStrips - 1) / kChannelStrips;
+    l.rows = want / kKeep * kKeep > least ? want / kKeep * kKeep : (least + kKeep - 1) / kKeep * kKeep;
+    l.rows = l.rows < kKeep ? kKeep : l.rows > kMostRows ? kMostRows : l.rows;
     l.strips = a.tokens > 0 ? (a.tokens + l.rows - 1) / l.rows : 1;
     const size_t slots = (size_t)l.strips * l.cut.blocks * l.V * kWave;
     l.words = 0;
     l.states = l.words + slots * sizeof(u64);
     l.partial = l.states + slots * sizeof(float);
-    l.bytes = l.partial + (back && l.cut.parts > 1 ? (size_t)l.cut.parts * a.tokens * a.heads * sizeof(float) : 0);
+    l.bytes = l.partial + (l.cut.parts > 1 ? (size_t)l.cut.parts * a.tokens * a.heads * sizeof(float) : 0);
     return l;
 }
 bool scan_fits(int dtype, const ScanArgs &a)        // launches of less than 2^32 threads
 {
-    for (const bool back : {false, true}) {
-        const Layout l = lay_out(dtype, a, back);
-        if (l.strips * l.cut.blocks >= ((int64_t)1 << 26) - kStripWaves || l.cut.blocks * l.V * kWave >= ((int64_t)1 << 25)) return false;
-    }
-    return true;
+    const Layout l = lay_out(dtype, a);
+    return l.strips * l.cut.blocks < ((int64_t)1 << 26) - kStripWaves && l.cut.blocks * l.V * kWave < ((int64_t)1 << 25);
 }
-size_t scan_scratch_bytes(int dtype, const ScanArgs &a)
-{
-    const size_t forward = lay_out(dtype, a, false).bytes, backward = lay_out(dtype, a, true).bytes;
-    return forward > backward ? forward : backward;
-}
+size_t scan_scratch_bytes(int dtype, const ScanArgs &a) { return lay_out(dtype, a).bytes; }
 
 static dim3 grid_of(const ScanArgs &a) { return dim3((unsigned)((a.strips * a.blocks + kStripWaves - 1) / kStripWaves)); }
 static void scan_states(const ScanArgs &a, int V, bool back, hipStream_t s)
 {
     const int64_t slots = a.blocks * V * kWave;
-    hipLaunchKernelGGL(k_scan_states, dim3((unsigned)(slots / kSlots)), dim3(kSlots * kPieces), 0, s, a.words, a.states, a.strips, slots, back);
+    const dim3 grid((unsigned)(slots / kSlots)), threads(kSlots * kPieces);
+    if (a.strips <= 8 * kPieces) hipLaunchKernelGGL(k_scan_states<8>, grid, threads, 0, s, a.words, a.states, a.strips, slots, back);
+    else if (a.strips <= 16 * kPieces) hipLaunchKernelGGL(k_scan_states<16>, grid, threads, 0, s, a.words, a.states, a.strips, slots, back);
+    else hipLaunchKernelGGL(k_scan_states<0>, grid, threads, 0, s, a.words, a.states, a.strips, slots, back);
 }
 template <class T, int kKind, int V, bool kShared> static void go_forward(const ScanArgs &a, hipStream_t s)
 {
@@ -683,9 +721,14 @@ template <class T, int kKind, int V, bool kShared> static void go_backward(const
         hipLaunchKernelGGL((k_gate_sums<T>), dim3((unsigned)(n < 8192 ? n : 8192)), dim3(256), 0, s, a);
     }
 }
+template <class T, int kKind, int V, bool kShared> static void go_scan(bool back, const ScanArgs &a, hipStream_t s)
+{
+    if (back) go_backward<T, kKind, V, kShared>(a, s);
+    else go_forward<T, kKind, V, kShared>(a, s);
+}
 template <class T, int kKind> static hipError_t go(int dtype, bool back, ScanArgs a, void *scratch, hipStream_t s)
 {
-    const Layout l = lay_out(dtype, a, back);
+    const Layout l = lay_out(dtype, a);
     char *mem = static_cast<char *>(scratch);
     a.blocks = l.cut.blocks;
     a.width = l.cut.width;
@@ -695,18 +738,13 @@ template <class T, int kKind> static hipError_t go(int dtype, bool back, ScanArg
     a.partial = reinterpret_cast<float *>(mem + l.partial);
     a.words = reinterpret_cast<u64 *>(mem + l.words);
     if (a.strips > kFewStrips) a.states = reinterpret_cast<float *>(mem + l.states);
-    constexpr bool kWide = sizeof(typename T::Store) == 4;
-    constexpr int kForward = kWide ? 2 : 4, kBackward = kWide ? 1 : 2;      // elements of a lane, at most
+    constexpr int kMost = sizeof(typename T::Store) == 4 ? 1 : 2;
     if (a.group == 1) {
-        if (back) { if (l.V == 1) go_backward<T, kKind, 1, false>(a, s); else go_backward<T, kKind, kBackward, false>(a, s); }
-        else if (l.V == 1) go_forward<T, kKind, 1, false>(a, s);
-        else if (l.V == 2) go_forward<T, kKind, 2, false>(a, s);
-        else go_forward<T, kKind, kForward, false>(a, s);
+        if (l.V == 1) go_scan<T, kKind, 1, false>(back, a, s);
+        else go_scan<T, kKind, kMost, false>(back, a, s);
     } else {
-        if (back) { if (l.V == 1) go_backward<T, kKind, 1, true>(a, s); else go_backward<T, kKind, kBackward, true>(a, s); }
-        else if (l.V == 1) go_forward<T, kKind, 1, true>(a, s);
-        else if (l.V == 2) go_forward<T, kKind, 2, true>(a, s);
-        else go_forward<T, kKind, kForward, true>(a, s);
+        if (l.V == 1) go_scan<T, kKind, 1, true>(back, a, s);
+        else go_scan<T, kKind, kMost, true>(back, a, s);
     }
     return hipGetLastError();
 }
