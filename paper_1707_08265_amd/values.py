@@ -23,19 +23,24 @@ def _need(ok, where):
         raise b.DgnError(b.DGN_ERR_INVALID_ARG, where)
 
 
-def _rows(t, rows, width, dtype, device, where):
-    """Address and row stride of a matrix whose rows have no gaps inside."""
-    _need(isinstance(t, torch.Tensor) and t.dtype is dtype and t.device == device and t.dim() == 2
-          and t.shape[0] == rows and t.shape[1] == width and (t.stride(1) == 1 or width <= 1)
-          and (t.stride(0) >= width or rows <= 1), where)
-    return t.data_ptr(), t.stride(0) if rows > 1 else 0
+def _rows(t, shape, dtype, index, where):
+    """Address and row stride of a matrix on GPU ``index`` whose rows have no gaps inside.  (Few questions to a tensor, each
+    costs 50 to 200 ns: a call for a few tokens is as long as what is asked here and its launch.)"""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != shape or t.get_device() != index:
+        raise b.DgnError(b.DGN_ERR_INVALID_ARG, where)
+    rows, width = shape
+    step, inner = t.stride()
+    if (inner != 1 and width > 1) or (step < width and rows > 1):
+        raise b.DgnError(b.DGN_ERR_INVALID_ARG, where)
+    return t.data_ptr(), step if rows > 1 else 0
 
 
-def _dense(t, shape, dtype, device, where):
+def _dense(t, shape, dtype, index, where):
     if t is None:
         return None
-    _need(isinstance(t, torch.Tensor) and t.dtype is dtype and t.device == device and tuple(t.shape) == shape
-          and t.is_contiguous(), where)
+    if (not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != shape or t.get_device() != index
+            or not t.is_contiguous()):
+        raise b.DgnError(b.DGN_ERR_INVALID_ARG, where)
     return t.data_ptr()
 
 
@@ -62,7 +67,9 @@ class ScanBuffers:
         new = lambda *shape, dtype=dtype: torch.zeros(shape, dtype=dtype, device=device)  # noqa: E731
         self.y = new(num_tokens, num_channels)
         self.final = new(num_seqs, num_channels, dtype=torch.float32)
-        self.device = self.y.device
+        self.device, self._index = self.y.device, self.y.get_device()
+        self._wide, self._gates = (num_tokens, num_channels), (num_tokens, self.num_heads)
+        self._ptr, self._states = (num_seqs + 1,), (num_seqs, num_channels)
         self._scratch, self._scratch_bytes = torch.empty(sb, dtype=torch.uint8, device=device), sb
         self._carry = torch.empty(cb, dtype=torch.uint8, device=device) if train else None
         if train:
@@ -70,11 +77,11 @@ class ScanBuffers:
             self.dh0 = new(num_seqs, num_channels, dtype=torch.float32)
 
     def _inputs(self, x, gate, seq_rowptr, h0):
-        d, dev = self._d, self.device
-        px, d.x_stride = _rows(x, self.num_tokens, self.num_channels, self.dtype, dev, "x")
-        pg, d.gate_stride = _rows(gate, self.num_tokens, self.num_heads, self.dtype, dev, "gate")
-        pr = _dense(seq_rowptr, (self.num_seqs + 1,), torch.int64, dev, "seq_rowptr")
-        return px, pg, pr, _dense(h0, (self.num_seqs, self.num_channels), torch.float32, dev, "h0")
+        d, at = self._d, self._index
+        px, d.x_stride = _rows(x, self._wide, self.dtype, at, "x")
+        pg, d.gate_stride = _rows(gate, self._gates, self.dtype, at, "gate")
+        pr = _dense(seq_rowptr, self._ptr, torch.int64, at, "seq_rowptr")
+        return px, pg, pr, _dense(h0, self._states, torch.float32, at, "h0")
 
     def forward(self, x, gate, seq_rowptr, h0=None, stream=None):
         """``x`` [tokens, channels], ``gate`` [tokens, heads], ``seq_rowptr`` int64 [seqs + 1], ``h0`` float [seqs, channels]."""
@@ -87,8 +94,8 @@ class ScanBuffers:
         """Gradients for ``dy`` [tokens, channels] and ``dfinal`` float [seqs, channels] of the last ``forward``."""
         _need(self.train, "backward of buffers made without train")
         px, pg, pr, ph = self._inputs(x, gate, seq_rowptr, h0)
-        py, self._d.dy_stride = _rows(dy, self.num_tokens, self.num_channels, self.dtype, self.device, "dy")
-        pf = _dense(dfinal, (self.num_seqs, self.num_channels), torch.float32, self.device, "dfinal")
+        py, self._d.dy_stride = _rows(dy, self._wide, self.dtype, self._index, "dy")
+        pf = _dense(dfinal, self._states, torch.float32, self._index, "dfinal")
         b._check(b._lib.dgn_scan_backward(ctypes.byref(self._d), px, pg, pr, ph, b._dp(self._carry), py, pf,
                                           self.dx.data_ptr(), self.dgate.data_ptr(), self.dh0.data_ptr(),
                                           self._scratch.data_ptr(), self._scratch_bytes, b._stream(stream)),
@@ -104,17 +111,19 @@ class ScanStepBuffers:
         self.num_rows, self.num_slots, self.num_channels = num_rows, num_slots, num_channels
         self.num_heads, self.dtype = num_channels // gate_group, dtype
         self.y = torch.empty(num_rows, num_channels, dtype=dtype, device=device)
-        self.device = self.y.device
+        self.device, self._index = self.y.device, self.y.get_device()
+        self._wide, self._gates = (num_rows, num_channels), (num_rows, self.num_heads)
+        self._one, self._pool = (num_rows,), (num_slots, num_channels)
 
     def step(self, x, gate, slots, state_in, state_out=None, stream=None):
         """Row r takes its state from row ``slots[r]`` of ``state_in`` (float [slots, channels]) and leaves it in the same
         row of ``state_out`` (default: ``state_in`` itself).  ``slots``: int32, -1 for an idle row, or None: row r."""
-        d, dev, pool = self._d, self.device, (self.num_slots, self.num_channels)
-        px, d.x_stride = _rows(x, self.num_rows, self.num_channels, self.dtype, dev, "x")
-        pg, d.gate_stride = _rows(gate, self.num_rows, self.num_heads, self.dtype, dev, "gate")
-        ps = _dense(slots, (self.num_rows,), torch.int32, dev, "slots")
-        pi = _dense(state_in, pool, torch.float32, dev, "state_in")
-        po = pi if state_out is None else _dense(state_out, pool, torch.float32, dev, "state_out")
+        d, at = self._d, self._index
+        px, d.x_stride = _rows(x, self._wide, self.dtype, at, "x")
+        pg, d.gate_stride = _rows(gate, self._gates, self.dtype, at, "gate")
+        ps = _dense(slots, self._one, torch.int32, at, "slots")
+        pi = _dense(state_in, self._pool, torch.float32, at, "state_in")
+        po = pi if state_out is None else _dense(state_out, self._pool, torch.float32, at, "state_out")
         b._check(b._lib.dgn_scan_step(ctypes.byref(d), self.num_slots, px, pg, ps, pi, po, self.y.data_ptr(), b._stream(stream)),
                  "dgn_scan_step")
 
@@ -126,10 +135,11 @@ class TensorList:
         self.tensors = list(tensors)
         n = len(self.tensors)
         dev = self.tensors[0].device if n else torch.device("cuda", torch.cuda.current_device())
+        self.device, self.index = dev, dev.index if dev.type == "cuda" else -1
         for t in self.tensors:
-            if not (isinstance(t, torch.Tensor) and t.dtype in DTYPES and t.is_contiguous() and t.device == dev):
+            if (not isinstance(t, torch.Tensor) or t.dtype not in DTYPES or t.get_device() != self.index or self.index < 0
+                    or not t.is_contiguous()):
                 raise b.DgnError(b.DGN_ERR_INVALID_ARG, "TensorList")
-        self.device = dev
         self._numel = np.fromiter((t.numel() for t in self.tensors), np.int64, n)
         data = np.fromiter((t.data_ptr() for t in self.tensors), np.uint64, n)
         types = np.fromiter((DTYPES[t.dtype] for t in self.tensors), np.int32, n)
@@ -144,9 +154,9 @@ class TensorList:
     def __len__(self):
         return len(self.tensors)
 
-    def close(self):
+    def close(self, destroy=b._lib.dgn_list_destroy):      # (bound here: a list may outlive the module's names)
         if self.handle:
-            b.dgn_list_destroy(self.handle)
+            destroy(self.handle)
             self.handle = None
 
     def __del__(self):
@@ -154,12 +164,18 @@ class TensorList:
             self.close()
 
 
-def _reach(lst, num_sets, mask, ids):
-    _need(ids is None or mask is not None, "tensor_ids without tensor_mask")
+def _fill_reach(r, lst, num_sets, mask, ids):
+    """``r``: the owner's own structure, filled for this call."""
+    r.num_sets = num_sets
     if mask is None:
-        return b.dgn_reach(num_sets, None, 0, None)
-    _need(mask.dtype is torch.int64 and mask.dim() == 1 and mask.is_contiguous() and mask.device == lst.device, "tensor_mask")
-    return b.dgn_reach(num_sets, mask.data_ptr(), mask.numel(), _dense(ids, (len(lst),), torch.int32, lst.device, "tensor_ids"))
+        _need(ids is None, "tensor_ids without tensor_mask")
+        r.tensor_mask, r.num_words, r.tensor_ids = None, 0, None
+        return
+    at = lst.index
+    if mask.dtype is not torch.int64 or mask.dim() != 1 or mask.get_device() != at or not mask.is_contiguous():
+        raise b.DgnError(b.DGN_ERR_INVALID_ARG, "tensor_mask")
+    r.tensor_mask, r.num_words = mask.data_ptr(), mask.numel()
+    r.tensor_ids = _dense(ids, (len(lst),), torch.int32, at, "tensor_ids")
 
 
 class GradientBuffers:
@@ -175,17 +191,20 @@ class GradientBuffers:
         b._check(rc, "dgn_list_norms_workspace")
         self.norms = torch.empty(max(num_sets, 1), dtype=torch.float32, device=grads.device)
         self._scratch, self._scratch_bytes = torch.empty(sb, dtype=torch.uint8, device=grads.device), sb
+        self._reach = b.dgn_reach()
 
     def norm(self, mask=None, ids=None, stream=None):
         """Fills ``norms`` [num_sets]."""
-        r = _reach(self.grads, self.num_sets, mask, ids)
+        r = self._reach
+        _fill_reach(r, self.grads, self.num_sets, mask, ids)
         b._check(b._lib.dgn_list_norms(self.grads.handle, ctypes.byref(r), self.norms.data_ptr(), self._scratch.data_ptr(),
                                        self._scratch_bytes, b._stream(stream)), "dgn_list_norms")
 
     def clip(self, out: TensorList, max_norm, eps=1e-6, mask=None, ids=None, stream=None):
         """Writes the gradients, scaled so that no set's norm is above ``max_norm``, to ``out`` (may be the list itself);
         goes by ``norms`` as the last ``norm`` call left them."""
-        r = _reach(self.grads, self.num_sets, mask, ids)
+        r = self._reach
+        _fill_reach(r, self.grads, self.num_sets, mask, ids)
         b._check(b._lib.dgn_list_clip(self.grads.handle, out.handle, ctypes.byref(r), self.norms.data_ptr(), max_norm, eps,
                                       b._stream(stream)), "dgn_list_clip")
 
@@ -198,6 +217,7 @@ class AdamBuffers:
                  out_v=None, copy=None):
         self._all = (grads, params, m, v, out_params, out_m, out_v, copy)
         self.grads = grads
+        self._reach = b.dgn_reach()
         self._lists = b.dgn_adam_lists(*(None if t is None else t.handle for t in self._all))
 
     def step(self, lr, beta1, beta2, eps, weight_decay, step, norms=None, max_norm=1.0, clip_eps=1e-6, mask=None, ids=None,
@@ -206,8 +226,9 @@ class AdamBuffers:
         if norms is not None:
             num_sets = norms.numel() if num_sets is None else num_sets
             _need(norms.dtype is torch.float32 and norms.is_contiguous() and norms.numel() >= num_sets
-                  and norms.device == self.grads.device, "norms")
-        r = _reach(self.grads, (64 if mask is not None else 1) if num_sets is None else num_sets, mask, ids)
+                  and norms.get_device() == self.grads.index, "norms")
+        r = self._reach
+        _fill_reach(r, self.grads, (64 if mask is not None else 1) if num_sets is None else num_sets, mask, ids)
         o = b.dgn_adam_options(lr, beta1, beta2, eps, weight_decay, step, int(skip_nonfinite), max_norm, clip_eps)
         b._check(b._lib.dgn_list_adam(ctypes.byref(self._lists), ctypes.byref(r), None if norms is None else norms.data_ptr(),
                                       ctypes.byref(o), b._stream(stream)), "dgn_list_adam")

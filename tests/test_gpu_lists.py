@@ -238,6 +238,35 @@ def test_many_tensors_and_one_large_one(dgn):
         assert ((b.norms.double().cpu() - want).abs() <= 2.0**-23 * want).all()
 
 
+def test_results_past_the_caches(dgn):
+    """Lists so large that their results are written past the caches, against the same elements in small lists (whose are not): the
+    arithmetic of an element is the same, so are its bits."""
+    n, piece = 40_000_007, 1_000_000
+    torch.manual_seed(3)
+    g = (torch.randn(n, device="cuda") * 0.01).to(torch.bfloat16)
+    p, m, v = (torch.randn(n, device="cuda") * 0.01 for _ in range(3))
+    v.square_()
+    b = dgn.GradientBuffers(dgn.TensorList([g, p]))
+    b.norm()
+    want = vo.norms([g, p], [1, 1], 1)
+    assert abs(float(b.norms[0]) - float(want[0])) <= 2.0**-23 * float(want[0])
+    out = [torch.empty_like(t) for t in (g, p)]
+    b.clip(dgn.TensorList(out), 3.0)
+    new, copy = [torch.empty_like(t) for t in (p, m, v)], torch.empty_like(g)
+    dgn.AdamBuffers(*(dgn.TensorList([t]) for t in (g, p, m, v)), *(dgn.TensorList([t]) for t in new),
+                    copy=dgn.TensorList([copy])).step(**ADAM, norms=b.norms, max_norm=3.0)
+    for at in (0, 17 * piece + 3, n - piece):
+        cut = [t[at:at + piece] for t in (g, p, m, v)]
+        few = dgn.GradientBuffers(dgn.TensorList(cut[:2]))
+        few.norms.copy_(b.norms)
+        small = [torch.empty_like(t) for t in (*cut, cut[0])]
+        few.clip(dgn.TensorList(small[:2]), 3.0)
+        assert all(torch.equal(o[at:at + piece], s) for o, s in zip(out, small)), at
+        dgn.AdamBuffers(*(dgn.TensorList([t]) for t in cut), *(dgn.TensorList([t]) for t in small[1:4]),
+                        copy=dgn.TensorList([small[4]])).step(**ADAM, norms=b.norms, max_norm=3.0)
+        assert all(torch.equal(o[at:at + piece], s) for o, s in zip((*new, copy), small[1:])), at
+
+
 def test_captured_graph_and_another_stream(dgn):
     g, out = tensors(), tensors(seed=5)
     lst, to = dgn.TensorList(g), dgn.TensorList(out)

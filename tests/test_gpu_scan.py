@@ -119,6 +119,43 @@ def test_what_is_no_number_stays_in_its_sequence_and_channel(dgn):
             assert torch.equal(got, value), (name, bad)
 
 
+def test_thousands_of_short_sequences(dgn):
+    check(dgn, make([0, 1, 2] * 1500, 6, 1, "sigmoid", "bf16"), 6, 1, "sigmoid", "bf16", "thousands")
+    check(dgn, make([1] * 30 + [0] * 4300 + [2, 0, 0], 70, 1, "decay", "f32"), 70, 1, "decay", "f32", "thousands empty")
+
+
+@pytest.mark.parametrize("heads,group", [(2048, 1), (16, 128)])
+def test_results_past_the_caches(dgn, heads, group):
+    """Calls so large that their results are written past the caches, against each sequence alone (whose are not), on random
+    rows.  Both round the same 32-bit values, cut in other places, to bf16: half a unit in the last place each, and the
+    32-bit values differ by far less."""
+    lens = [30000, 1, 0, 9999]
+    n, c = sum(lens), heads * group
+    torch.manual_seed(5)
+    rn = lambda w: torch.randn(n, w, device="cuda").to(torch.bfloat16)  # noqa: E731
+    x, gate, dy = rn(c), (rn(heads) * 1.5 + 2.0), rn(c)
+    ptr = torch.tensor([0, 30000, 30001, 30001, n], device="cuda")
+    b = dgn.ScanBuffers(n, 4, c, gate_group=group, kind="sigmoid", train=True)
+    b.forward(x, gate, ptr)
+    b.backward(x, gate, ptr, dy)
+    for q, m in enumerate(lens):
+        at, step = slice(int(ptr[q]), int(ptr[q]) + m), 64
+        for head in (0, heads // 2):                     # a few heads of each sequence, so that the call is small
+            few = max(1, step // group)
+            h, ch = slice(head, head + few), slice(head * group, (head + few) * group)
+            o = dgn.ScanBuffers(m, 1, few * group, gate_group=group, kind="sigmoid", train=True)
+            one = torch.tensor([0, m], device="cuda")
+            args = (x[at, ch], gate[at, h], one)
+            o.forward(*args)
+            o.backward(*args, dy[at, ch])
+            for name, cols in (("y", ch), ("dx", ch), ("dgate", h)):
+                got, want = getattr(b, name)[at, cols].float(), getattr(o, name).float()
+                scale = want.abs().clamp(min=1e-2) if group == 1 else want.abs() + 1e-2 * group ** 0.5
+                assert ((got - want).abs() <= 2.0 ** -7 * scale).all(), (name, q, head)
+            torch.testing.assert_close(b.final[q, ch], o.final[0], rtol=1e-4, atol=1e-4)
+            torch.testing.assert_close(b.dh0[q, ch], o.dh0[0], rtol=1e-4, atol=1e-4)
+
+
 def test_long_sequences_and_repeats(dgn):
     """Longer than anything that one workgroup sees, twice: the same bits; many channels beside."""
     for kind, dtype, n, heads, group in [("sigmoid", "bf16", 9001, 6, 1), ("decay", "f32", 5000, 2, 130), ("decay", "f16", 7001, 3, 64)]:
