@@ -292,29 +292,15 @@ struct Rows {
 };
 
 
-// First launch: the links of the strips.  kBack: of the gradients, where (A, B) of rows 0 .. n-1 is what comes back from a row after
-// them: A the product of their gates, B the sum of dy_k times the gates up to k.
-template <class T, int kKind, int V, bool kShared, bool kBack>
-__global__ __launch_bounds__(kStripWaves *kWave, 8) void k_scan_links(ScanArgs a)
-{
+// Rows k0 .. k0 + 7 of a strip in two arrays.
+template <class T, int V, bool kShared> struct Batch {
     typedef typename T::Store S;
-    constexpr int kTokens = 8;
-    __shared__ Marks s_marks[kStripWaves];
-    Marks &marks = s_marks[wave_id()];
-    Strip<V, kShared> st;
-    const int64_t number = (int64_t)blockIdx.x * kStripWaves + wave_id();
-    if (!st.find(a, number, false)) return;
-    st.mark(a, marks);
-    const S *in = static_cast<const S *>(kBack ? a.dy : a.x);
-    const int64_t in_stride = kBack ? a.dy_stride : a.x_stride;
-    float A[V], h[V];
-#pragma unroll
-    for (int i = 0; i < V; i++) { A[i] = 1.0f; h[i] = 0.0f; }
-    bool cut = false;
-    for (int k0 = 0; k0 < st.rows; k0 += kTokens) {
-        Pack<T, V> x[kTokens];
-        Pack<T, kShared ? 1 : V> g[kTokens];
-        Rows xs(st.row0 + k0, a.tokens, in_stride, st.c), gs(st.row0 + k0, a.tokens, a.gate_stride, kShared ? st.head0 : st.c);
+    static constexpr int kTokens = 8;
+    Pack<T, V> x[kTokens];
+    Pack<T, kShared ? 1 : V> g[kTokens];
+    __device__ __forceinline__ void load(const ScanArgs &a, const Strip<V, kShared> &st, const S *in, int64_t stride, int k0)
+    {
+        Rows xs(st.row0 + k0, a.tokens, stride, st.c), gs(st.row0 + k0, a.tokens, a.gate_stride, kShared ? st.head0 : st.c);
 #pragma unroll
         for (int k = 0; k < kTokens; k++) {
             x[k].load(in + xs.at + st.mine);
@@ -322,36 +308,78 @@ __global__ __launch_bounds__(kStripWaves *kWave, 8) void k_scan_links(ScanArgs a
             xs.next(k);
             gs.next(k);
         }
-        const Row16 at = marks_of<kTokens>(kBack ? marks.end : marks.begin, st.marked, k0);
-#pragma unroll
-        for (int k = 0; k < kTokens; k++) {
-            if (k0 + k >= st.rows) break;
-            const bool here = at.bits >> k & 1;
-            if (!kBack && here) {
-                load_state<V>(row_of(a.h0, __builtin_amdgcn_readlane(at.id, k), a, st.c), st.mine, h);
-                cut = true;
-            }
-            float ga, gb;
-#pragma unroll
-            for (int i = 0; i < V; i++) {
-                if (!kShared || i == 0) open_gate<kKind>(g[k].get(i), ga, gb);
-                A[i] *= ga;
-                h[i] = kBack ? fmaf(A[i], x[k].get(i), h[i]) : fmaf(ga, h[i], gb * x[k].get(i));
-            }
-            if (kBack && here) {
-                float d[V];
-                load_state<V>(row_of(a.dfinal, __builtin_amdgcn_readlane(at.id, k), a, st.c), st.mine, d);
-#pragma unroll
-                for (int i = 0; i < V; i++) h[i] = fmaf(A[i], d[i], h[i]);
-                cut = true;
-                break;                                  // (what comes after it is another sequence's)
-            }
-        }
-        if (kBack && cut) break;
     }
+};
+
+// The link of a strip.  kBack: of the gradients, where (A, B) of rows 0 .. n-1 is what comes back from a row after them: A the product of
+// their gates, B the sum of dy_k times the gates up to k.
+template <class T, int kKind, int V, bool kShared, bool kBack>
+__device__ __forceinline__ void strip_link(const ScanArgs &a, Strip<V, kShared> &st, Marks &marks, u64 (&link)[V])
+{
+    typedef typename T::Store S;
+    constexpr int kTokens = Batch<T, V, kShared>::kTokens;
+    const S *in = static_cast<const S *>(kBack ? a.dy : a.x);
+    const int64_t stride = kBack ? a.dy_stride : a.x_stride;
+    float A[V], h[V];
+#pragma unroll
+    for (int i = 0; i < V; i++) { A[i] = 1.0f; h[i] = 0.0f; }
+    bool cut = false;
+    Batch<T, V, kShared> now, next;
+    if (st.rows > 0) now.load(a, st, in, stride, 0);
+    st.mark(a, marks);                                  // (with the first rows on their way)
+    for (int k0 = 0; k0 < st.rows; k0 += kTokens) {
+        if (k0 + kTokens < st.rows) next.load(a, st, in, stride, k0 + kTokens);
+        const Row16 at = marks_of<kTokens>(kBack ? marks.end : marks.begin, st.marked, k0);
+        const auto rows = [&](auto some) {
+#pragma unroll
+            for (int k = 0; k < kTokens; k++) {
+                if (some.value && k0 + k >= st.rows) break;
+                const bool here = some.value && (at.bits >> k & 1);
+                if (!kBack && here) {
+                    load_state<V>(row_of(a.h0, __builtin_amdgcn_readlane(at.id, k), a, st.c), st.mine, h);
+                    cut = true;
+                }
+                float ga, gb;
+#pragma unroll
+                for (int i = 0; i < V; i++) {
+                    if (!kShared || i == 0) open_gate<kKind>(now.g[k].get(i), ga, gb);
+                    A[i] *= ga;
+                    h[i] = kBack ? fmaf(A[i], now.x[k].get(i), h[i]) : fmaf(ga, h[i], gb * now.x[k].get(i));
+                }
+                if (kBack && here) {
+                    float d[V];
+                    load_state<V>(row_of(a.dfinal, __builtin_amdgcn_readlane(at.id, k), a, st.c), st.mine, d);
+#pragma unroll
+                    for (int i = 0; i < V; i++) h[i] = fmaf(A[i], d[i], h[i]);
+                    cut = true;
+                    break;                              // (what comes after it is another sequence's)
+                }
+            }
+        };
+        // (most rows are in the middle of a sequence: those ask for nothing, so that the next ones can stay on their way)
+        if (at.bits == 0 && k0 + kTokens <= st.rows) rows(std::false_type());
+        else rows(std::true_type());
+        if (kBack && cut) break;
+        now = next;
+    }
+#pragma unroll
+    for (int i = 0; i < V; i++) link[i] = link_word(A[i], h[i], cut);
+}
+
+// First launch: the links of the strips.
+template <class T, int kKind, int V, bool kShared, bool kBack>
+__global__ __launch_bounds__(kStripWaves *kWave, 8) void k_scan_links(ScanArgs a)
+{
+    __shared__ Marks s_marks[kStripWaves];
+    Marks &marks = s_marks[wave_id()];
+    Strip<V, kShared> st;
+    const int64_t number = (int64_t)blockIdx.x * kStripWaves + wave_id();
+    if (!st.find(a, number, false)) return;
+    u64 link[V];
+    strip_link<T, kKind, V, kShared, kBack>(a, st, marks, link);
     u64 *out = a.words + number * (kWave * V) + lane_id() * V;
 #pragma unroll
-    for (int i = 0; i < V; i++) out[i] = link_word(A[i], h[i], cut);
+    for (int i = 0; i < V; i++) out[i] = link[i];
 }
 
 // Second launch: the state that comes into each strip, states[strip][slot].  A workgroup has kSlots slots; the strips are cut into kPieces
@@ -421,32 +449,18 @@ template <int V> __device__ __forceinline__ void state_before(const ScanArgs &a,
     }
 }
 
-// Third launch, forward.  The strips from the last to the first: what the first launch read last is still in the cache.
-template <class T, int kKind, int V, bool kShared, bool kStream>
-__global__ __launch_bounds__(kStripWaves *kWave, 8) void k_scan_outputs(ScanArgs a)
+// The outputs of a strip, from the state that comes into it.  kMarked: its marks are there.
+template <class T, int kKind, int V, bool kShared, bool kStream, bool kMarked>
+__device__ __forceinline__ void strip_outputs(const ScanArgs &a, Strip<V, kShared> &st, Marks &marks, float (&h)[V])
 {
     typedef typename T::Store S;
-    constexpr int kTokens = 8;
-    __shared__ Marks s_marks[kStripWaves];
-    Marks &marks = s_marks[wave_id()];
-    Strip<V, kShared> st;
-    if (!st.find(a, (int64_t)blockIdx.x * kStripWaves + wave_id(), true)) return;
-    float h[V];
-    state_before<V>(a, st.strip, st.number, false, h);
-    st.mark(a, marks);
-    if (st.empties && a.final) st.copy_empties(a, a.h0, a.final);
+    constexpr int kTokens = Batch<T, V, kShared>::kTokens;
+    if (!kMarked && st.rows == 0) st.mark(a, marks);
     S *y = static_cast<S *>(a.y) + st.row0 * a.y_stride + st.c;
     for (int k0 = 0; k0 < st.rows; k0 += kTokens) {
-        Pack<T, V> x[kTokens];
-        Pack<T, kShared ? 1 : V> g[kTokens];
-        Rows xs(st.row0 + k0, a.tokens, a.x_stride, st.c), gs(st.row0 + k0, a.tokens, a.gate_stride, kShared ? st.head0 : st.c);
-#pragma unroll
-        for (int k = 0; k < kTokens; k++) {
-            x[k].load(static_cast<const S *>(a.x) + xs.at + st.mine);
-            g[k].load(static_cast<const S *>(a.gate) + gs.at + (kShared ? st.head : st.mine));
-            xs.next(k);
-            gs.next(k);
-        }
+        Batch<T, V, kShared> now;
+        now.load(a, st, static_cast<const S *>(a.x), a.x_stride, k0);
+        if (!kMarked && k0 == 0) st.mark(a, marks);     // (with the first rows on their way)
         const Row16 begin = marks_of<kTokens>(marks.begin, st.marked, k0), end = marks_of<kTokens>(marks.end, st.marked, k0);
         if (a.kept && (st.row0 + k0) % kKeep == 0) store_state<V>(a.kept + (st.row0 + k0) / kKeep * a.channels + st.c, st.mine, h);
 #pragma unroll
@@ -455,8 +469,8 @@ __global__ __launch_bounds__(kStripWaves *kWave, 8) void k_scan_outputs(ScanArgs
             float ga, gb;
 #pragma unroll
             for (int i = 0; i < V; i++) {
-                if (!kShared || i == 0) open_gate<kKind>(g[k].get(i), ga, gb);
-                h[i] = fmaf(ga, h[i], gb * x[k].get(i));
+                if (!kShared || i == 0) open_gate<kKind>(now.g[k].get(i), ga, gb);
+                h[i] = fmaf(ga, h[i], gb * now.x[k].get(i));
             }
             if (k0 + k >= st.from && k0 + k < st.to) {
                 Pack<T, V> out;
@@ -467,6 +481,20 @@ __global__ __launch_bounds__(kStripWaves *kWave, 8) void k_scan_outputs(ScanArgs
             if ((end.bits >> k & 1) && a.final) store_state<V>(row_of(a.final, __builtin_amdgcn_readlane(end.id, k), a, st.c), st.mine, h);
         }
     }
+    if (st.empties && a.final) st.copy_empties(a, a.h0, a.final);
+}
+
+// Third launch, forward.  The strips from the last to the first: what the first launch read last is still in the cache.
+template <class T, int kKind, int V, bool kShared, bool kStream>
+__global__ __launch_bounds__(kStripWaves *kWave, 8) void k_scan_outputs(ScanArgs a)
+{
+    __shared__ Marks s_marks[kStripWaves];
+    Marks &marks = s_marks[wave_id()];
+    Strip<V, kShared> st;
+    if (!st.find(a, (int64_t)blockIdx.x * kStripWaves + wave_id(), true)) return;
+    float h[V];
+    state_before<V>(a, st.strip, st.number, false, h);
+    strip_outputs<T, kKind, V, kShared, kStream, false>(a, st, marks, h);
 }
 
 // Sums of N values a lane (of rows `row` ...) over groups of 2 d lanes, handed to write(row, sum) by one lane of each.  At each step two lanes
@@ -504,20 +532,13 @@ template <int N, class F> __device__ __forceinline__ void sum_any_lanes(float (&
     for (int k = 0; k < N; k++) if (writes && at == 0) write(k, v[k]);
 }
 
-// Third launch, backward.  kKeep rows at a time, the last first: the states before each of them from the one that is kept, then the gradients.
+// The gradients of a strip, from what comes back into it.  kKeep rows at a time, the last first: the states before each of them from the
+// one that is kept, then the gradients.  sums: room for a wave's [kKeep][kWave] (shared gates).
 template <class T, int kKind, int V, bool kShared, bool kStream>
-__global__ __launch_bounds__(kStripWaves *kWave, 4) void k_scan_gradients(ScanArgs a)
+__device__ __forceinline__ void strip_gradients(const ScanArgs &a, const Strip<V, kShared> &st, const Marks &marks, float *sums, float (&e)[V])
 {
     typedef typename T::Store S;
     constexpr int kTokens = kKeep;
-    __shared__ Marks s_marks[kStripWaves];
-    Marks &marks = s_marks[wave_id()];
-    __shared__ float s_sums[kShared ? kStripWaves : 1][kShared ? kTokens * kWave : 1];
-    Strip<V, kShared> st;
-    if (!st.find(a, (int64_t)blockIdx.x * kStripWaves + wave_id(), true)) return;
-    float e[V];
-    state_before<V>(a, st.strip, st.number, true, e);
-    st.mark(a, marks);
     if (st.empties && a.dh0) st.copy_empties(a, a.dfinal, a.dh0);
     for (int k0 = (st.rows - 1) / kTokens * kTokens; k0 >= 0 && st.rows > 0; k0 -= kTokens) {
         Pack<T, V> x[kTokens], dy[kTokens];
@@ -590,8 +611,7 @@ __global__ __launch_bounds__(kStripWaves *kWave, 4) void k_scan_gradients(ScanAr
                 for (int k = 0; k < kTokens; k++) sum[k] = 0.0f;
             }
             const int lanes = a.parts > 1 ? kWave : (int)(a.group / V);
-            float *sums = s_sums[wave_id()];            // [row][head of the block]
-            const auto write = [&](int k, float v) { sums[k * kWave + st.head] = v; };
+            const auto write = [&](int k, float v) { sums[k * kWave + st.head] = v; };     // [row][head of the block]
             const bool writes = st.active || a.parts > 1;
             if ((lanes & (lanes - 1)) == 0) sum_lanes<kTokens>(sum, lanes >> 1, 0, writes, write);
             else sum_any_lanes<kTokens>(sum, lanes, writes, write);
@@ -607,6 +627,54 @@ __global__ __launch_bounds__(kStripWaves *kWave, 4) void k_scan_gradients(ScanAr
             wave_fence();
         }
     }
+}
+
+// Third launch, backward.
+template <class T, int kKind, int V, bool kShared, bool kStream>
+__global__ __launch_bounds__(kStripWaves *kWave, 4) void k_scan_gradients(ScanArgs a)
+{
+    __shared__ Marks s_marks[kStripWaves];
+    __shared__ float s_sums[kShared ? kStripWaves : 1][kShared ? kKeep * kWave : 1];
+    Marks &marks = s_marks[wave_id()];
+    Strip<V, kShared> st;
+    if (!st.find(a, (int64_t)blockIdx.x * kStripWaves + wave_id(), true)) return;
+    float e[V];
+    state_before<V>(a, st.strip, st.number, true, e);
+    st.mark(a, marks);
+    strip_gradients<T, kKind, V, kShared, kStream>(a, st, marks, s_sums[kShared ? wave_id() : 0], e);
+}
+
+// Short calls in one launch: a workgroup has all strips of its channels, a wave to a strip, and the links stay in LDS.  (16 x 512 forward 6.6
+// us, in two launches 9.8; 128 rows 9.3 and 11.3.  With 16 waves, 256 rows, 13.0 and 12.3: one compute unit does then what many could.)
+constexpr int kShortWaves = 8;
+template <class T, int kKind, int V, bool kShared, bool kBack>
+__global__ __launch_bounds__(kShortWaves *kWave) void k_scan_short(ScanArgs a)
+{
+    __shared__ Marks s_marks[kShortWaves];
+    __shared__ u64 s_link[kShortWaves][V][kWave];
+    __shared__ float s_sums[kShared && kBack ? kShortWaves : 1][kShared && kBack ? kKeep * kWave : 1];
+    const int wave = wave_id(), lane = lane_id(), strips = (int)a.strips;
+    Marks &marks = s_marks[wave];
+    Strip<V, kShared> st;
+    st.find(a, wave * a.blocks + blockIdx.x, false);        // (as many waves as strips)
+    if (strips == 1) st.mark(a, marks);
+    else {
+        u64 link[V];
+        strip_link<T, kKind, V, kShared, kBack>(a, st, marks, link);
+#pragma unroll
+        for (int i = 0; i < V; i++) s_link[wave][i][lane] = link[i];
+        __syncthreads();
+    }
+    float h[V];
+#pragma unroll
+    for (int i = 0; i < V; i++) h[i] = 0.0f;
+    const int before = kBack ? strips - 1 - wave : wave;
+    for (int n = 0; n < before; n++) {
+#pragma unroll
+        for (int i = 0; i < V; i++) h[i] = apply_word(s_link[kBack ? strips - 1 - n : n][i][lane], h[i]);
+    }
+    if constexpr (kBack) strip_gradients<T, kKind, V, kShared, false>(a, st, marks, s_sums[kShared ? wave : 0], h);
+    else strip_outputs<T, kKind, V, kShared, false, true>(a, st, marks, h);
 }
 
 // Gates shared by more channels than a wave has: the sum of the parts' sums.
@@ -700,9 +768,19 @@ static void scan_states(const ScanArgs &a, int V, bool back, hipStream_t s)
     else if (a.strips <= 16 * kPieces) hipLaunchKernelGGL(k_scan_states<16>, grid, threads, 0, s, a.words, a.states, a.strips, slots, back);
     else hipLaunchKernelGGL(k_scan_states<0>, grid, threads, 0, s, a.words, a.states, a.strips, slots, back);
 }
+template <class T> static void gate_sums(const ScanArgs &a, hipStream_t s)
+{
+    if (a.parts == 1 || a.tokens == 0) return;
+    const int64_t n = (a.tokens * a.heads + 255) / 256;
+    hipLaunchKernelGGL((k_gate_sums<T>), dim3((unsigned)(n < 8192 ? n : 8192)), dim3(256), 0, s, a);
+}
 template <class T, int kKind, int V, bool kShared> static void go_forward(const ScanArgs &a, hipStream_t s)
 {
-    if (a.strips > 1) hipLaunchKernelGGL((k_scan_links<T, kKind, V, kShared, false>), grid_of(a), dim3(kStripWaves * kWave), 0, s, a);
+    if (a.strips <= kShortWaves) {
+        hipLaunchKernelGGL((k_scan_short<T, kKind, V, kShared, false>), dim3((unsigned)a.blocks), dim3((unsigned)a.strips * kWave), 0, s, a);
+        return;
+    }
+    hipLaunchKernelGGL((k_scan_links<T, kKind, V, kShared, false>), grid_of(a), dim3(kStripWaves * kWave), 0, s, a);
     if (a.states) scan_states(a, V, false, s);
     // x, gate and y; x, gate, dy, dx and dgate (of the backward pass)
     if (a.tokens * (2 * a.channels + a.heads) * sizeof(typename T::Store) > kStreamBytes)
@@ -711,15 +789,17 @@ template <class T, int kKind, int V, bool kShared> static void go_forward(const 
 }
 template <class T, int kKind, int V, bool kShared> static void go_backward(const ScanArgs &a, hipStream_t s)
 {
-    if (a.strips > 1) hipLaunchKernelGGL((k_scan_links<T, kKind, V, kShared, true>), grid_of(a), dim3(kStripWaves * kWave), 0, s, a);
+    if (a.strips <= kShortWaves) {
+        hipLaunchKernelGGL((k_scan_short<T, kKind, V, kShared, true>), dim3((unsigned)a.blocks), dim3((unsigned)a.strips * kWave), 0, s, a);
+        gate_sums<T>(a, s);
+        return;
+    }
+    hipLaunchKernelGGL((k_scan_links<T, kKind, V, kShared, true>), grid_of(a), dim3(kStripWaves * kWave), 0, s, a);
     if (a.states) scan_states(a, V, true, s);
     if (a.tokens * (3 * a.channels + 2 * a.heads) * sizeof(typename T::Store) > kStreamBytes)
         hipLaunchKernelGGL((k_scan_gradients<T, kKind, V, kShared, true>), grid_of(a), dim3(kStripWaves * kWave), 0, s, a);
     else hipLaunchKernelGGL((k_scan_gradients<T, kKind, V, kShared, false>), grid_of(a), dim3(kStripWaves * kWave), 0, s, a);
-    if (a.parts > 1 && a.tokens > 0) {
-        const int64_t n = (a.tokens * a.heads + 255) / 256;
-        hipLaunchKernelGGL((k_gate_sums<T>), dim3((unsigned)(n < 8192 ? n : 8192)), dim3(256), 0, s, a);
-    }
+    gate_sums<T>(a, s);
 }
 template <class T, int kKind, int V, bool kShared> static void go_scan(bool back, const ScanArgs &a, hipStream_t s)
 {
