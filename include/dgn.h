@@ -442,6 +442,9 @@ int dgn_selftest_wave_ops(void *buffer, size_t bytes, dgn_stream stream);
 
 /* ---- values of tensors: what a pruned training step runs next ------------------------------------- */
 
+/* These calls only enqueue: none waits, copies to the host or allocates (dgn_list_build does), so they can be
+ * captured into a HIP graph. */
+
 /* Element types.  Whatever the type, arithmetic is in 32 bits or more and a result is rounded once, when it is
  * stored (to nearest, ties to even). */
 enum { DGN_F32 = 0, DGN_F16 = 1, DGN_BF16 = 2 };
@@ -456,7 +459,9 @@ enum { DGN_F32 = 0, DGN_F16 = 1, DGN_BF16 = 2 };
  * empty).  Rows before the first and after the last sequence are neither read nor written, so buffers may have room
  * for more tokens than a batch has.  The lengths are never asked for on the host.  Row pointers that do not ascend
  * give unspecified values; rows outside 0..num_tokens are not touched.
- * A state that is no finite number stays none in its own sequence and channel and reaches no other. */
+ * A state that is no finite number stays none in its own sequence and channel and reaches no other.  Products of up to
+ * 64 gates of a channel are formed and have to be in the range of floats, as they are for decays of magnitude up to 1.
+ * Sizes whose launches would hold 2^32 threads or more are refused (DGN_ERR_TOO_LARGE). */
 enum { DGN_GATE_DECAY = 0, DGN_GATE_SIGMOID = 1 };
 
 typedef struct dgn_scan_desc {

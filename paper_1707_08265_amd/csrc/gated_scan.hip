@@ -11,7 +11,8 @@
 // The rows, whatever sequences they belong to, are cut into strips; a wave takes a strip of 64 V channels.  What a strip does to the state
 // that comes into it is h -> A h + B (A the product of its gates, B its end from a state of zero), or h -> B if a sequence begins in it.
 // Three launches: the strips' (A, B); the states between strips, a short scan per channel; the strips again, now with the state that comes
-// into each.  Nothing waits for anything within a launch, and the order of all sums is given by the sizes alone.
+// into each (two launches for up to 512 rows, one for up to 128).  Nothing waits for anything within a launch, and the order of all sums
+// is given by the sizes alone.  It is bound by memory: forward every element of x and gate is read twice, of gate and dy backward.
 // (In one launch, that reads x and gate once, a workgroup keeps its rows in registers until the workgroups before it have handed their state
 // on.  All of them then load, wait and store at the same time: 65 301 x 2 048 forward in f16 253 us, 10 000 x 1 000 43 us, training step of
 // 65 537 x 1 024 500 us.)
@@ -138,7 +139,6 @@ __device__ __forceinline__ Block block_of(const ScanArgs &a, int64_t block)
     const int64_t head = divide(block, a.parts), part = block - head * a.parts, at = part * a.width, left = a.group - at;
     return Block{head * a.group + at, (int32_t)(left < a.width ? left : a.width), (int32_t)part};
 }
-
 
 constexpr int kKeep = kScanKeep;        // rows between two states that the forward pass keeps for the backward pass
 constexpr int kMostRows = 64;           // rows of a strip, at most
@@ -291,7 +291,6 @@ struct Rows {
     __device__ __forceinline__ void next(int k) { at += k < left ? stride : 0; }
 };
 
-
 // Rows k0 .. k0 + 7 of a strip in two arrays.
 template <class T, int V, bool kShared> struct Batch {
     typedef typename T::Store S;
@@ -366,7 +365,7 @@ __device__ __forceinline__ void strip_link(const ScanArgs &a, Strip<V, kShared> 
     for (int i = 0; i < V; i++) link[i] = link_word(A[i], h[i], cut);
 }
 
-// First launch: the links of the strips.
+// First launch: the links of the strips.  65 537 x 1 024 in bf16: 268 MB in 55 us, 4.9 TB/s (a large copy: 4.8).
 template <class T, int kKind, int V, bool kShared, bool kBack>
 __global__ __launch_bounds__(kStripWaves *kWave, 8) void k_scan_links(ScanArgs a)
 {
@@ -484,7 +483,8 @@ __device__ __forceinline__ void strip_outputs(const ScanArgs &a, Strip<V, kShare
     if (st.empties && a.final) st.copy_empties(a, a.h0, a.final);
 }
 
-// Third launch, forward.  The strips from the last to the first: what the first launch read last is still in the cache.
+// Third launch, forward.  The strips from the last to the first: what the first launch read last is still in the cache, and results of calls
+// larger than it go past it.  65 537 x 1 024 in bf16: 402 MB in 74 us, 5.4 TB/s.
 template <class T, int kKind, int V, bool kShared, bool kStream>
 __global__ __launch_bounds__(kStripWaves *kWave, 8) void k_scan_outputs(ScanArgs a)
 {
@@ -629,7 +629,8 @@ __device__ __forceinline__ void strip_gradients(const ScanArgs &a, const Strip<V
     }
 }
 
-// Third launch, backward.
+// Third launch, backward: 65 537 x 1 024 in bf16, 688 MB in 137 us, 5.0 TB/s.  Four waves to a SIMD: with five or six, and registers spilled,
+// the training step takes 409 and 474 us instead of 318.
 template <class T, int kKind, int V, bool kShared, bool kStream>
 __global__ __launch_bounds__(kStripWaves *kWave, 4) void k_scan_gradients(ScanArgs a)
 {
@@ -690,7 +691,8 @@ __global__ __launch_bounds__(256) void k_gate_sums(ScanArgs a)
     }
 }
 
-// One token: a row of the batch is cut into pieces of 256 V channels, a workgroup each.
+// One token: a row of the batch is cut into pieces of 256 V channels, a workgroup each.  Bound by memory, and for few rows by the launch: 4 096
+// rows of 2 048 channels 18.5 us, 5.3 TB/s, with four channels a thread; 32.8 us with one.
 template <class T, int kKind, int V, bool kShared>
 __global__ __launch_bounds__(256) void k_scan_step(StepArgs a)
 {

@@ -1,5 +1,9 @@
 // Operators over a list of tensors: norms of up to 64 target sets, clipping by them, and the update that applies it.
-// A tensor is cut into chunks of kListChunk elements; a workgroup takes one.
+//   n_q = sqrt(sum of |g_i|^2 over the tensors i of set q),   f_i = min over its sets of min(1, max_norm / (n_q + eps))
+//   m' = beta1 m + (1 - beta1) f g,   v' = beta2 v + (1 - beta2) (f g)^2,   p' = p - lr (m' / c1 / (sqrt(v' / c2) + eps) + wd p)
+// A tensor is cut into chunks of kListChunk elements, which a list has a table of: address, size and type in one load.  All of it is
+// bound by memory.  500 layers of 120 M elements in all: squares of bf16 240 MB in 48 us, 5.0 TB/s; clipping 480 MB in 74 us, 6.5 TB/s, with
+// half of what it reads still in the cache; the update 3.4 GB in 600 us, 5.6 TB/s (a large copy: 4.8).
 #include "values.h"
 
 namespace dgn {
@@ -102,7 +106,10 @@ __device__ __forceinline__ u64 reach_of(const Reach &r, int32_t entry)
     return at >= 0 && at < r.words ? r.mask[at] & all : 0;
 }
 
-constexpr int kListThreads = 256, kClipParts = 2;      // (parts: workgroups to a chunk)
+// Threads of a workgroup, and workgroups to a chunk.  The update goes over nine arrays at once, and is the faster the closer together all
+// workgroups are in them: one pass of 2 048 elements each 657 us, of 1 024 690 us, four passes of 1 024 750 us or, from the last
+// chunk to the first, 812.
+constexpr int kListThreads = 256, kClipParts = 2;
 constexpr int kAdamThreads = 512, kAdamParts = 4;
 
 // Squares are added up in 64 bits: those of 32-bit gradients above 2e19 or below 1e-23 have no 32-bit value.
