@@ -2,8 +2,8 @@
 //   n_q = sqrt(sum of |g_i|^2 over the tensors i of set q),   f_i = min over its sets of min(1, max_norm / (n_q + eps))
 //   m' = beta1 m + (1 - beta1) f g,   v' = beta2 v + (1 - beta2) (f g)^2,   p' = p - lr (m' / c1 / (sqrt(v' / c2) + eps) + wd p)
 // A tensor is cut into chunks of kListChunk elements, which a list has a table of: address, size and type in one load.  All of it is
-// bound by memory.  500 layers of 120 M elements in all: squares of bf16 240 MB in 48 us, 5.0 TB/s; clipping 480 MB in 74 us, 6.5 TB/s, with
-// half of what it reads still in the cache; the update 3.4 GB in 600 us, 5.6 TB/s (a large copy: 4.8).
+// bound by memory.  500 layers of 120 M elements in all: squares of bf16 240 MB in 42 us, 5.7 TB/s; clipping 482 MB in 77 us, 6.3 TB/s;
+// the update 3.37 GB in 604 to 623 us, 5.4 to 5.6 TB/s (a copy by a thread per 16 bytes: 6.2, past the caches 6.5).
 #include "values.h"
 
 namespace dgn {
