@@ -481,7 +481,8 @@ int dgn_scan_workspace(const dgn_scan_desc *desc, size_t *scratch_bytes, size_t 
 /* x [num_tokens][num_channels], gate [num_tokens][num_channels / gate_group], h0 float [num_seqs][num_channels] or
  * NULL -> y [num_tokens][num_channels], final float [num_seqs][num_channels] or NULL (the state after the last token;
  * h0 of an empty sequence), carry: carry_bytes for dgn_scan_backward, or NULL.  All DEVICE, aligned to their
- * elements; scratch to 8 bytes.  y may not overlap x or gate. */
+ * elements; scratch to 8 bytes.  y may not overlap x or gate.  final may be h0, or overlap it (sequences that go on from call
+ * to call: h0 is then copied first; a backward pass needs the states that were there before). */
 int dgn_scan_forward(const dgn_scan_desc *desc, const void *x, const void *gate, const int64_t *seq_rowptr,
                      const float *h0, void *y, float *final, void *carry, void *scratch, size_t scratch_bytes,
                      dgn_stream stream);
@@ -489,7 +490,7 @@ int dgn_scan_forward(const dgn_scan_desc *desc, const void *x, const void *gate,
 /* Gradients for dy [num_tokens][num_channels] and dfinal float [num_seqs][num_channels] (or NULL: zero): dx, dgate (a
  * shared gate's is the sum over its channels) and dh0 float (or NULL: not asked for).  x, gate, seq_rowptr and h0 as
  * dgn_scan_forward had them, carry as it left it.  The states are computed again from there in 32 bits, so y is not
- * needed.  The same inputs give the same bits. */
+ * needed.  dh0 may be dfinal, or overlap it (dfinal is then copied first).  The same inputs give the same bits. */
 int dgn_scan_backward(const dgn_scan_desc *desc, const void *x, const void *gate, const int64_t *seq_rowptr,
                       const float *h0, const void *carry, const void *dy, const float *dfinal, void *dx, void *dgate,
                       float *dh0, void *scratch, size_t scratch_bytes, dgn_stream stream);

@@ -691,6 +691,12 @@ __global__ __launch_bounds__(256) void k_gate_sums(ScanArgs a)
     }
 }
 
+// A copy of the states that come in, for calls whose states go out to the same memory: strips read and write them in any order.
+__global__ __launch_bounds__(256) void k_copy_states(const float *from, float *to, int64_t n)
+{
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) to[i] = from[i];
+}
+
 // One token: a row of the batch is cut into pieces of 256 V channels, a workgroup each.  Bound by memory, and for few rows by the launch: 4 096
 // rows of 2 048 channels 18.5 us, 5.3 TB/s, with four channels a thread; 32.8 us with one.
 template <class T, int kKind, int V, bool kShared>
@@ -737,7 +743,7 @@ static int elements_of(int dtype, const ScanArgs &a)
 // more strips than the second launch keeps in registers -- from kKeep to kMostRows.
 constexpr int64_t kStrips = 8192, kChannelStrips = 1024;
 constexpr int64_t kFewStrips = 32;      // up to here a strip applies the links before it itself: 257 x 512 forward 14.6 us instead of 16.6
-struct Layout { int V; Cut cut; int64_t rows, strips; size_t words, states, partial, bytes; };
+struct Layout { int V; Cut cut; int64_t rows, strips; size_t words, states, partial, before, bytes; };
 static Layout lay_out(int dtype, const ScanArgs &a)
 {
     Layout l;
@@ -751,7 +757,8 @@ static Layout lay_out(int dtype, const ScanArgs &a)
     l.words = 0;
     l.states = l.words + slots * sizeof(u64);
     l.partial = l.states + slots * sizeof(float);
-    l.bytes = l.partial + (l.cut.parts > 1 ? (size_t)l.cut.parts * a.tokens * a.heads * sizeof(float) : 0);
+    l.before = l.partial + (l.cut.parts > 1 ? (size_t)l.cut.parts * a.tokens * a.heads * sizeof(float) : 0);
+    l.bytes = l.before + (size_t)a.seqs * a.channels * sizeof(float);
     return l;
 }
 bool scan_fits(int dtype, const ScanArgs &a)        // launches of less than 2^32 threads
@@ -820,6 +827,15 @@ template <class T, int kKind> static hipError_t go(int dtype, bool back, ScanArg
     a.partial = reinterpret_cast<float *>(mem + l.partial);
     a.words = reinterpret_cast<u64 *>(mem + l.words);
     if (a.strips > kFewStrips) a.states = reinterpret_cast<float *>(mem + l.states);
+    const float *&in = back ? a.dfinal : a.h0;
+    const float *out = back ? a.dh0 : a.final;
+    const int64_t n = a.seqs * a.channels;
+    if (in && out && in < out + n && out < in + n) {
+        float *copy = reinterpret_cast<float *>(mem + l.before);
+        const int64_t groups = (n + 255) / 256;
+        hipLaunchKernelGGL(k_copy_states, dim3((unsigned)(groups < 4096 ? groups : 4096)), dim3(256), 0, s, in, copy, n);
+        in = copy;
+    }
     constexpr int kMost = sizeof(typename T::Store) == 4 ? 1 : 2;
     if (a.group == 1) {
         if (l.V == 1) go_scan<T, kKind, 1, false>(back, a, s);

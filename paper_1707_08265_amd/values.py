@@ -84,16 +84,20 @@ class ScanBuffers:
         return px, pg, pr, _dense(h0, self._states, torch.float32, at, "h0")
 
     def forward(self, x, gate, seq_rowptr, h0=None, stream=None):
-        """``x`` [tokens, channels], ``gate`` [tokens, heads], ``seq_rowptr`` int64 [seqs + 1], ``h0`` float [seqs, channels]."""
+        """``x`` [tokens, channels], ``gate`` [tokens, heads], ``seq_rowptr`` int64 [seqs + 1], ``h0`` float [seqs, channels]:
+        may be ``final`` itself, for sequences that go on from call to call."""
         px, pg, pr, ph = self._inputs(x, gate, seq_rowptr, h0)
         b._check(b._lib.dgn_scan_forward(ctypes.byref(self._d), px, pg, pr, ph, self.y.data_ptr(), self.final.data_ptr(),
                                          b._dp(self._carry), self._scratch.data_ptr(), self._scratch_bytes,
                                          b._stream(stream)), "dgn_scan_forward")
 
     def backward(self, x, gate, seq_rowptr, dy, h0=None, dfinal=None, stream=None):
-        """Gradients for ``dy`` [tokens, channels] and ``dfinal`` float [seqs, channels] of the last ``forward``."""
+        """Gradients for ``dy`` [tokens, channels] and ``dfinal`` float [seqs, channels] of the last ``forward``.  ``dfinal`` may be
+        ``dh0``; ``h0`` may not be ``final``, where ``forward`` has written since."""
         _need(self.train, "backward of buffers made without train")
         px, pg, pr, ph = self._inputs(x, gate, seq_rowptr, h0)
+        if ph:
+            _need(abs(ph - self.final.data_ptr()) >= 4 * self.num_seqs * self.num_channels, "h0 of backward: final has been written")
         py, self._d.dy_stride = _rows(dy, self._wide, self.dtype, self._index, "dy")
         pf = _dense(dfinal, self._states, torch.float32, self._index, "dfinal")
         b._check(b._lib.dgn_scan_backward(ctypes.byref(self._d), px, pg, pr, ph, b._dp(self._carry), py, pf,
