@@ -92,7 +92,7 @@ template <class T, int V> struct Pack {
 
 // What a run of rows does to the state that comes into it: A h + B, or B alone if `cut` (a sequence begins in it, or for gradients ends).
 // In memory: B in the low half, A in the high one (an A that is no number as the usual one, and as another to say `cut`).
-constexpr uint32_t kNaN = 0x7fc00000u, kCut = 0x7fc00001u;
+constexpr uint32_t kNaN = 0x7fc00000u, kCut = 0x7fc00001u, kWide = 0x7fc00002u;       // (kWide: see k_scan_states)
 __device__ __forceinline__ u64 link_word(float A, float B, bool cut)
 {
     const uint32_t bits = cut ? kCut : A != A ? kNaN : __float_as_uint(A);
@@ -385,37 +385,67 @@ __global__ __launch_bounds__(kStripWaves *kWave, 8) void k_scan_links(ScanArgs a
 // pieces, each is put together, the pieces' links are applied one after the other, and each is gone through again: with its words in
 // registers where they are few (kEach > 0: at most so many), so that they are asked for once and all at once: 625 strips of 1 024 slots 6.5
 // instead of 8.3 us.  (With 32 of them, for 1 025 strips, 16.7 us instead of 10.2: too many registers for 1 024 threads.)
+// A piece has any number of gates.  Products that only fall may reach 0; where one of the strips' is above 1, their product could pass the range
+// of floats though no state does (200 decays of 2, then 200 of 1/2): it is then held as a 64-bit fraction with an exponent beside it, and
+// applied in 64 bits.  (In 64 bits always: 3 us more.)
 constexpr int kSlots = 16, kPieces = 64;
 template <int kEach>
 __global__ __launch_bounds__(kSlots *kPieces) void k_scan_states(const u64 *words, float *states, int64_t strips, int64_t slots, bool back)
 {
     __shared__ u64 s_link[kPieces][kSlots];
+    __shared__ double s_wide[kPieces][kSlots];
     const int64_t slot = (int64_t)blockIdx.x * kSlots + threadIdx.x % kSlots;
     const int piece = threadIdx.x / kSlots;
     const int64_t each = (strips + kPieces - 1) / kPieces, from = piece * each, to = from + each < strips ? from + each : strips;
     const auto row = [&](int64_t n) { return (back ? strips - 1 - n : n) * slots + slot; };
     u64 kept[kEach > 0 ? kEach : 1];
     float A = 1.0f, B = 0.0f;
-    bool cut = false;
-    const auto join = [&](u64 w) {
-        B = apply_word(w, B);
-        A *= __uint_as_float((uint32_t)(w >> 32));
-        cut = cut || word_cuts(w);
-    };
+    bool cut = false, grows = false;
     if (kEach > 0) {
 #pragma unroll
         for (int k = 0; k < kEach; k++) kept[k] = from + k < to ? words[row(from + k)] : link_word(1.0f, 0.0f, false);
+    }
+    const auto every = [&](auto join) {
+        if (kEach > 0) {
 #pragma unroll
-        for (int k = 0; k < kEach; k++) join(kept[k]);
+            for (int k = 0; k < kEach; k++) join(kept[k]);
+        } else {
+#pragma unroll 8
+            for (int64_t n = from; n < to; n++) join(words[row(n)]);
+        }
+    };
+    every([&](u64 w) {
+        const float a = __uint_as_float((uint32_t)(w >> 32));
+        B = apply_word(w, B);
+        A *= a;
+        cut = cut || word_cuts(w);
+        grows = grows || !(fabsf(a) <= 1.0f);
+    });
+    u64 link = link_word(A, B, cut);
+    if (grows && !cut) {
+        double wide = 1.0;
+        int exponent = 0;
+        every([&](u64 w) {
+            wide *= (double)__uint_as_float((uint32_t)(w >> 32));
+            exponent += __builtin_amdgcn_frexp_exp(wide);
+            wide = __builtin_amdgcn_frexp_mant(wide);
+        });
+        // (from 2^1000 on every state but 0 is past the floats, from 2^-1000 down none is left)
+        s_wide[piece][threadIdx.x % kSlots] = ldexp(wide, exponent < -1000 ? -1000 : exponent > 1000 ? 1000 : exponent);
+        link = (u64)kWide << 32 | (uint32_t)link;
+    }
+    s_link[piece][threadIdx.x % kSlots] = link;
+    float h = 0.0f;
+    if (__syncthreads_or(grows && !cut)) {
+        for (int p = 0; p < piece; p++) {
+            const u64 w = s_link[p][threadIdx.x % kSlots];
+            if ((uint32_t)(w >> 32) == kWide) h = (float)fma(s_wide[p][threadIdx.x % kSlots], (double)h, (double)__uint_as_float((uint32_t)w));
+            else h = apply_word(w, h);
+        }
     } else {
 #pragma unroll 8
-        for (int64_t n = from; n < to; n++) join(words[row(n)]);
+        for (int p = 0; p < piece; p++) h = apply_word(s_link[p][threadIdx.x % kSlots], h);
     }
-    s_link[piece][threadIdx.x % kSlots] = link_word(A, B, cut);
-    __syncthreads();
-    float h = 0.0f;
-#pragma unroll 8
-    for (int p = 0; p < piece; p++) h = apply_word(s_link[p][threadIdx.x % kSlots], h);
     if (kEach > 0) {
 #pragma unroll
         for (int k = 0; k < kEach; k++) {

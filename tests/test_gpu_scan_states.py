@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from test_gpu_scan import TYPES, dgn, make  # noqa: F401
+from test_gpu_scan import TYPES, check, dgn, make  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 GOING_ON = [[40], [100], [129, 0, 1000, 5], [9000, 1, 0, 700]]      # one strip, one launch, two launches, three
@@ -75,3 +75,32 @@ def test_a_captured_call_goes_on_at_every_replay(dgn):  # noqa: F811
         assert torch.equal(b.y, eager.y) and torch.equal(b.final, eager.final), turn
         torch.testing.assert_close(b.y, whole.y[at], rtol=2e-5, atol=2e-5)
     torch.testing.assert_close(b.final, whole.final, rtol=2e-5, atol=2e-5)
+
+
+@pytest.mark.parametrize("n,middle,at", [(10000, 5000, 960), (20001, 13000, 3200), (66001, 40000, 8704)])
+def test_gates_whose_products_leave_the_range_of_floats(dgn, n, middle, at):  # noqa: F811
+    """Products of up to 64 gates are in range, those of more are not, and states and gradients are, forward and backward, with
+    sequences that begin in the middle; the last of the sizes has more than 1 024 strips of 64 rows."""
+    i = make([middle, 0, n - middle], 8, 1, "decay", "f32")
+    for name in ("x", "dy"):
+        i[name][:middle, :7] = 0.0
+    i["h0"][0, :7] = 0.0
+    i["dfinal"][0, :7] = 0.0
+    gate, tiny = i["gate"][:middle], 2.0 ** -60
+    gate[:, :7] = 1.0
+    gate[:, :2] = 0.5
+    gate[at:at + 64, 0] = 2.0                   # states of 0 stay 0 ...
+    gate[at:at + 160, 1] = 2.0                  # ... and here,
+    gate[:1200, 4] = 1.1                        # and here
+    for c, first in [(2, 2.0), (3, 2.0), (5, 0.5), (6, 0.5)]:
+        gate[at:at + 140, c], gate[at + 140:at + 280, c] = first, 1.0 / first
+    i["h0"][0, 2] = i["h0"][0, 3] = tiny         # states between 2^-60 and 2^80
+    i["dfinal"][0, 5] = i["dfinal"][0, 6] = tiny
+    gen = torch.Generator().manual_seed(1)
+    i["x"][:middle, 3] = (torch.randn(middle, generator=gen) * 2.0 ** -70).cuda()
+    i["dy"][:middle, 6] = (torch.randn(middle, generator=gen) * 2.0 ** -70).cuda()
+    b = check(dgn, i, 8, 1, "decay", "f32", "products")
+    for t in (b.y, b.dx, b.dgate):
+        assert (t[:middle, [0, 1, 4]] == 0).all()
+    assert float(b.y[:middle, 2].max()) == 2.0 ** 80 and float(b.final[0, 2]) == tiny
+    assert float(b.dx[:middle, 5].max()) == 2.0 ** 80 and float(b.dh0[0, 5]) == tiny
