@@ -536,8 +536,8 @@ int dgn_list_norms(const dgn_list *list, const dgn_reach *reach, float *norms, v
                    dgn_stream stream);
 
 /* out_i = f_i g_i, f_i the least of min(1, max_norm / (norms[q] + eps)) over the sets q that need tensor i, so that
- * afterwards no set's norm is above max_norm; 1 where none does.  A norm that is infinite gives 0, one that is NaN gives
- * NaN.  `out` has the sizes of `list` and may be `list` itself, or share single tensors with it. */
+ * afterwards no set's norm is above max_norm; 1 where none does, and for a set whose norm and eps are 0.  A norm that is
+ * infinite gives 0, also if max_norm is (which scales nothing else), one that is NaN gives NaN.  `out` has the sizes of `list` and may be `list` itself, or share single tensors with it. */
 int dgn_list_clip(const dgn_list *list, const dgn_list *out, const dgn_reach *reach, const float *norms, float max_norm,
                   float eps, dgn_stream stream);
 

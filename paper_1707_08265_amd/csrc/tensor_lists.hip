@@ -205,7 +205,8 @@ __device__ __forceinline__ float clip_factor(const ClipArgs &c, u64 bits, bool &
         const float n = c.norms[lane];
         fine = fabsf(n) < INFINITY;
         f = c.max_norm / (n + c.eps);
-        if (f > 1.0f) f = 1.0f;
+        if (f > 1.0f || n + c.eps <= 0.0f) f = 1.0f;        // (gradients of 0, and max_norm and eps as well: nothing to scale)
+        if (n == INFINITY) f = 0.0f;                        // (also if max_norm is infinite)
     }
     finite = __all(fine);
 #pragma unroll

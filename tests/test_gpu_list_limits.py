@@ -1,0 +1,43 @@
+"""Norms, clipping and update over lists at the limits of their arguments."""
+import pytest
+import torch
+
+from test_gpu_lists import ADAM, dgn, tensors  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+INF, NAN = float("inf"), float("nan")
+
+
+@pytest.mark.parametrize("norms,max_norm,eps,want", [
+    ([0.0, 0.0], 0.0, 0.0, [1.0, 1.0]),              # gradients of 0, nothing allowed: they stay 0
+    ([0.0, 2.0], 0.0, 0.0, [1.0, 0.0]),
+    ([0.0, 2.0], 1.0, 0.0, [1.0, 0.5]),
+    ([INF, 2.0], INF, 0.0, [0.0, 1.0]),              # an infinite limit scales nothing, but for a norm that is infinite
+    ([INF, NAN], INF, 1e-6, [0.0, NAN]),
+    ([INF, 1e30], 1.0, 1e-6, [0.0, 1e-30]),
+    ([NAN, 0.0], 0.0, 0.0, [NAN, 1.0]),
+])
+def test_factors_at_their_limits(dgn, norms, max_norm, eps, want):  # noqa: F811
+    """Clipping by given norms, and the update's own factors (its first moment from 0 is (1 - beta1) f g)."""
+    f32 = [torch.float32]
+    g = [t.fill_(1.0) for t in tensors([300, 5000], f32)]
+    out, words = tensors([300, 5000], f32, seed=1), torch.tensor([1, 2], device="cuda")
+    lst = dgn.TensorList(g)
+    b = dgn.GradientBuffers(lst, 2)
+    b.norms.copy_(torch.tensor(norms))
+    b.clip(dgn.TensorList(out), max_norm, eps=eps, mask=words)
+    p, m, v = ([t.zero_() for t in tensors([300, 5000], f32)] for _ in range(3))
+    dgn.AdamBuffers(lst, *(dgn.TensorList(t) for t in (p, m, v))).step(**ADAM, norms=b.norms, max_norm=max_norm, clip_eps=eps, mask=words)
+    for i, f in enumerate(want):
+        near = dict(rtol=2.0 ** -20, atol=0.0, equal_nan=True)
+        torch.testing.assert_close(out[i], torch.full_like(out[i], f), **near)
+        torch.testing.assert_close(m[i], torch.full_like(m[i], f * (1 - ADAM["beta1"])), **near)
+
+
+def test_gradients_of_zero_stay_zero_when_nothing_is_allowed(dgn):  # noqa: F811
+    g = [torch.zeros(n, device="cuda", dtype=torch.bfloat16) for n in (7, 5000)]
+    lst = dgn.TensorList(g)
+    b = dgn.GradientBuffers(lst)
+    b.norm()
+    b.clip(lst, 0.0, eps=0.0)
+    assert all((t == 0).all() for t in g)
