@@ -178,7 +178,8 @@ def _fill_reach(r, lst, num_sets, mask, ids):
     at = lst.index
     if mask.dtype is not torch.int64 or mask.dim() != 1 or mask.get_device() != at or not mask.is_contiguous():
         raise b.DgnError(b.DGN_ERR_INVALID_ARG, "tensor_mask")
-    r.tensor_mask, r.num_words = mask.data_ptr(), mask.numel()
+    # (a mask of no words has no address, which would say that there is no mask: the list's own is not read)
+    r.tensor_mask, r.num_words = mask.data_ptr() or lst._mem.data_ptr(), mask.numel()
     r.tensor_ids = _dense(ids, (len(lst),), torch.int32, at, "tensor_ids")
 
 

@@ -41,3 +41,23 @@ def test_gradients_of_zero_stay_zero_when_nothing_is_allowed(dgn):  # noqa: F811
     b.norm()
     b.clip(lst, 0.0, eps=0.0)
     assert all((t == 0).all() for t in g)
+
+
+def test_a_mask_of_no_words_reaches_nothing(dgn):  # noqa: F811
+    """The mask of a graph without tensors: ids lie outside of it, so no set needs any entry; without ids it is too short."""
+    f32 = [torch.float32]
+    g, p, m, v = (tensors([300, 5000], f32, seed=k) for k in range(4))
+    old = [t.clone() for ts in (g, p, m, v) for t in ts]
+    lst = dgn.TensorList(g)
+    empty, ids = torch.zeros(0, dtype=torch.int64, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    b = dgn.GradientBuffers(lst, 3)
+    a = dgn.AdamBuffers(lst, *(dgn.TensorList(t) for t in (p, m, v)))
+    b.norm(empty, ids)
+    assert (b.norms == 0).all()
+    b.norms.fill_(50.0)
+    b.clip(lst, 1.0, mask=empty, ids=ids)
+    a.step(**ADAM, mask=empty, ids=ids)
+    assert all(torch.equal(t, o) for t, o in zip([t for ts in (g, p, m, v) for t in ts], old))
+    for call in (lambda: b.norm(empty), lambda: b.clip(lst, 1.0, mask=empty), lambda: a.step(**ADAM, mask=empty)):
+        with pytest.raises(dgn.DgnError):
+            call()
