@@ -220,14 +220,21 @@ class AdamBuffers:
 
     def __init__(self, grads: TensorList, params: TensorList, m: TensorList, v: TensorList, out_params=None, out_m=None,
                  out_v=None, copy=None):
-        self._all = (grads, params, m, v, out_params, out_m, out_v, copy)
+        self._all = [t for t in (grads, params, m, v, out_params, out_m, out_v, copy) if t is not None]
+        self._need_open()
         self.grads = grads
         self._reach = b.dgn_reach()
-        self._lists = b.dgn_adam_lists(*(None if t is None else t.handle for t in self._all))
+        self._lists = b.dgn_adam_lists(*(None if t is None else t.handle for t in (grads, params, m, v, out_params, out_m, out_v, copy)))
+
+    def _need_open(self):       # (the library keeps nothing of a list that is closed, and takes none for `in place`)
+        for t in self._all:
+            if not t.handle:
+                raise b.DgnError(b.DGN_ERR_INVALID_ARG, "AdamBuffers: a closed list")
 
     def step(self, lr, beta1, beta2, eps, weight_decay, step, norms=None, max_norm=1.0, clip_eps=1e-6, mask=None, ids=None,
              num_sets=None, skip_nonfinite=False, stream=None):
         """``norms`` (of ``GradientBuffers``): gradients are scaled as ``clip`` would; ``num_sets`` defaults to their number."""
+        self._need_open()
         if norms is not None:
             num_sets = norms.numel() if num_sets is None else num_sets
             _need(norms.dtype is torch.float32 and norms.is_contiguous() and norms.numel() >= num_sets

@@ -1,6 +1,7 @@
 """What the owners of buffers hand to the library, without a GPU."""
 from types import SimpleNamespace
 
+import pytest
 import torch
 
 import paper_1707_08265_amd as dgn
@@ -12,3 +13,36 @@ def test_a_mask_of_no_words_is_still_a_mask():
     r = dgn.dgn_reach()
     values._fill_reach(r, lst, 1, torch.zeros(0, dtype=torch.int64), torch.zeros(2, dtype=torch.int32))
     assert r.num_words == 0 and r.tensor_mask and r.tensor_ids
+
+
+class Lists:
+    """Stand-ins for lists of tensors, and a library that notes what it is called with."""
+
+    def __init__(self, monkeypatch):
+        self.calls = []
+        note = lambda *a: self.calls.append(a) or 0  # noqa: E731
+        for name in ("dgn_list_adam", "dgn_list_clip", "dgn_list_norms"):
+            monkeypatch.setattr(values.b._lib, name, note)
+        monkeypatch.setattr(values.b, "_stream", lambda stream=None: 0)
+
+    def make(self, n=8, index=0):
+        return [SimpleNamespace(handle=1000 + i, index=index) for i in range(n)]
+
+
+ADAM = dict(lr=1e-2, beta1=0.9, beta2=0.95, eps=1e-8, weight_decay=0.1, step=3)
+
+
+@pytest.mark.parametrize("closed", range(8))
+def test_update_with_a_closed_list_is_refused(monkeypatch, closed):
+    """Closed after the owner was made: its handle is no longer the library's.  Before: an optional list is not `in place`."""
+    env = Lists(monkeypatch)
+    lists = env.make()
+    a = values.AdamBuffers(*lists)
+    a.step(**ADAM)
+    assert len(env.calls) == 1
+    lists[closed].handle = None
+    with pytest.raises(dgn.DgnError):
+        a.step(**ADAM)
+    with pytest.raises(dgn.DgnError):
+        values.AdamBuffers(*lists)
+    assert len(env.calls) == 1
