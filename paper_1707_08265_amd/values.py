@@ -68,6 +68,7 @@ class ScanBuffers:
         self.y = new(num_tokens, num_channels)
         self.final = new(num_seqs, num_channels, dtype=torch.float32)
         self.device, self._index = self.y.device, self.y.get_device()
+        _need(self._index >= 0, "device: not a GPU")
         self._wide, self._gates = (num_tokens, num_channels), (num_tokens, self.num_heads)
         self._ptr, self._states = (num_seqs + 1,), (num_seqs, num_channels)
         self._scratch, self._scratch_bytes = torch.empty(sb, dtype=torch.uint8, device=device), sb
@@ -116,6 +117,7 @@ class ScanStepBuffers:
         self.num_heads, self.dtype = num_channels // gate_group, dtype
         self.y = torch.empty(num_rows, num_channels, dtype=dtype, device=device)
         self.device, self._index = self.y.device, self.y.get_device()
+        _need(self._index >= 0, "device: not a GPU")
         self._wide, self._gates = (num_rows, num_channels), (num_rows, self.num_heads)
         self._one, self._pool = (num_rows,), (num_slots, num_channels)
 

@@ -46,3 +46,13 @@ def test_update_with_a_closed_list_is_refused(monkeypatch, closed):
     with pytest.raises(dgn.DgnError):
         values.AdamBuffers(*lists)
     assert len(env.calls) == 1
+
+
+def test_buffers_in_host_memory_are_refused():
+    """Kernels would be given host addresses: tensors of the same device as the buffers pass every later check."""
+    with pytest.raises(dgn.DgnError):
+        dgn.ScanBuffers(20, 2, 12, device="cpu")
+    with pytest.raises(dgn.DgnError):
+        dgn.ScanBuffers(20, 2, 12, train=True, device="cpu")
+    with pytest.raises(dgn.DgnError):
+        dgn.ScanStepBuffers(4, 8, 12, device="cpu")
