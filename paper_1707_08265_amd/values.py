@@ -18,9 +18,19 @@ DTYPES = {torch.float32: b.DGN_F32, torch.float16: b.DGN_F16, torch.bfloat16: b.
 GATES = {"decay": b.DGN_GATE_DECAY, "sigmoid": b.DGN_GATE_SIGMOID}
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _need(ok, where):
     if not ok:
         raise b.DgnError(b.DGN_ERR_INVALID_ARG, where)
+
+
+def _queue(index, stream):
+    """The stream to launch on: the current one, or ``stream``.  It and the current device have to be of GPU ``index``."""
+    if _current_device() != index or (stream is not None and isinstance(stream, torch.cuda.Stream) and stream.device_index != index):
+        raise b.DgnError(b.DGN_ERR_INVALID_ARG, "the current device or stream is not of the buffers' GPU")
+    return b._raw_stream(index) if stream is None and b._raw_stream is not None else b._stream(stream)
 
 
 def _rows(t, shape, dtype, index, where):
@@ -90,7 +100,7 @@ class ScanBuffers:
         px, pg, pr, ph = self._inputs(x, gate, seq_rowptr, h0)
         b._check(b._lib.dgn_scan_forward(ctypes.byref(self._d), px, pg, pr, ph, self.y.data_ptr(), self.final.data_ptr(),
                                          b._dp(self._carry), self._scratch.data_ptr(), self._scratch_bytes,
-                                         b._stream(stream)), "dgn_scan_forward")
+                                         _queue(self._index, stream)), "dgn_scan_forward")
 
     def backward(self, x, gate, seq_rowptr, dy, h0=None, dfinal=None, stream=None):
         """Gradients for ``dy`` [tokens, channels] and ``dfinal`` float [seqs, channels] of the last ``forward``.  ``dfinal`` may be
@@ -103,7 +113,7 @@ class ScanBuffers:
         pf = _dense(dfinal, self._states, torch.float32, self._index, "dfinal")
         b._check(b._lib.dgn_scan_backward(ctypes.byref(self._d), px, pg, pr, ph, b._dp(self._carry), py, pf,
                                           self.dx.data_ptr(), self.dgate.data_ptr(), self.dh0.data_ptr(),
-                                          self._scratch.data_ptr(), self._scratch_bytes, b._stream(stream)),
+                                          self._scratch.data_ptr(), self._scratch_bytes, _queue(self._index, stream)),
                  "dgn_scan_backward")
 
 
@@ -130,7 +140,7 @@ class ScanStepBuffers:
         ps = _dense(slots, self._one, torch.int32, at, "slots")
         pi = _dense(state_in, self._pool, torch.float32, at, "state_in")
         po = pi if state_out is None else _dense(state_out, self._pool, torch.float32, at, "state_out")
-        b._check(b._lib.dgn_scan_step(ctypes.byref(d), self.num_slots, px, pg, ps, pi, po, self.y.data_ptr(), b._stream(stream)),
+        b._check(b._lib.dgn_scan_step(ctypes.byref(d), self.num_slots, px, pg, ps, pi, po, self.y.data_ptr(), _queue(self._index, stream)),
                  "dgn_scan_step")
 
 
@@ -154,7 +164,7 @@ class TensorList:
         rc, nb = b.dgn_list_workspace(desc)
         b._check(rc, "dgn_list_workspace")
         self._mem = torch.empty(nb, dtype=torch.uint8, device=dev)
-        rc, self.handle = b.dgn_list_build(desc, self._mem, nb, stream)
+        rc, self.handle = b.dgn_list_build(desc, self._mem, nb, _queue(self.index, stream))
         b._check(rc, "dgn_list_build")
 
     def __len__(self):
@@ -205,15 +215,17 @@ class GradientBuffers:
         r = self._reach
         _fill_reach(r, self.grads, self.num_sets, mask, ids)
         b._check(b._lib.dgn_list_norms(self.grads.handle, ctypes.byref(r), self.norms.data_ptr(), self._scratch.data_ptr(),
-                                       self._scratch_bytes, b._stream(stream)), "dgn_list_norms")
+                                       self._scratch_bytes, _queue(self.grads.index, stream)), "dgn_list_norms")
 
     def clip(self, out: TensorList, max_norm, eps=1e-6, mask=None, ids=None, stream=None):
         """Writes the gradients, scaled so that no set's norm is above ``max_norm``, to ``out`` (may be the list itself);
         goes by ``norms`` as the last ``norm`` call left them."""
-        r = self._reach
+        at, r = self.grads.index, self._reach
+        if out.index != at:
+            raise b.DgnError(b.DGN_ERR_INVALID_ARG, "clip: a list of another device")
         _fill_reach(r, self.grads, self.num_sets, mask, ids)
         b._check(b._lib.dgn_list_clip(self.grads.handle, out.handle, ctypes.byref(r), self.norms.data_ptr(), max_norm, eps,
-                                      b._stream(stream)), "dgn_list_clip")
+                                      _queue(at, stream)), "dgn_list_clip")
 
 
 class AdamBuffers:
@@ -224,14 +236,14 @@ class AdamBuffers:
                  out_v=None, copy=None):
         self._all = [t for t in (grads, params, m, v, out_params, out_m, out_v, copy) if t is not None]
         self._need_open()
+        _need(all(t.index == grads.index for t in self._all), "AdamBuffers: lists of several devices")
         self.grads = grads
         self._reach = b.dgn_reach()
         self._lists = b.dgn_adam_lists(*(None if t is None else t.handle for t in (grads, params, m, v, out_params, out_m, out_v, copy)))
 
     def _need_open(self):       # (the library keeps nothing of a list that is closed, and takes none for `in place`)
-        for t in self._all:
-            if not t.handle:
-                raise b.DgnError(b.DGN_ERR_INVALID_ARG, "AdamBuffers: a closed list")
+        if None in [t.handle for t in self._all]:
+            raise b.DgnError(b.DGN_ERR_INVALID_ARG, "AdamBuffers: a closed list")
 
     def step(self, lr, beta1, beta2, eps, weight_decay, step, norms=None, max_norm=1.0, clip_eps=1e-6, mask=None, ids=None,
              num_sets=None, skip_nonfinite=False, stream=None):
@@ -245,4 +257,4 @@ class AdamBuffers:
         _fill_reach(r, self.grads, (64 if mask is not None else 1) if num_sets is None else num_sets, mask, ids)
         o = b.dgn_adam_options(lr, beta1, beta2, eps, weight_decay, step, int(skip_nonfinite), max_norm, clip_eps)
         b._check(b._lib.dgn_list_adam(ctypes.byref(self._lists), ctypes.byref(r), None if norms is None else norms.data_ptr(),
-                                      ctypes.byref(o), b._stream(stream)), "dgn_list_adam")
+                                      ctypes.byref(o), _queue(self.grads.index, stream)), "dgn_list_adam")

@@ -23,7 +23,8 @@ class Lists:
         note = lambda *a: self.calls.append(a) or 0  # noqa: E731
         for name in ("dgn_list_adam", "dgn_list_clip", "dgn_list_norms"):
             monkeypatch.setattr(values.b._lib, name, note)
-        monkeypatch.setattr(values.b, "_stream", lambda stream=None: 0)
+        monkeypatch.setattr(values, "_current_device", lambda: 0)
+        monkeypatch.setattr(values.b, "_raw_stream", lambda index: 0)
 
     def make(self, n=8, index=0):
         return [SimpleNamespace(handle=1000 + i, index=index) for i in range(n)]
@@ -56,3 +57,29 @@ def test_buffers_in_host_memory_are_refused():
         dgn.ScanBuffers(20, 2, 12, train=True, device="cpu")
     with pytest.raises(dgn.DgnError):
         dgn.ScanStepBuffers(4, 8, 12, device="cpu")
+
+
+@pytest.mark.parametrize("other", range(1, 8))
+def test_lists_of_another_device_are_refused(monkeypatch, other):
+    env = Lists(monkeypatch)
+    lists = env.make()
+    lists[other].index = 1
+    with pytest.raises(dgn.DgnError):
+        values.AdamBuffers(*lists)
+    norms = values.GradientBuffers.__new__(values.GradientBuffers)
+    norms.grads, norms.num_sets, norms._reach, norms.norms = lists[0], 1, dgn.dgn_reach(), torch.zeros(1)
+    norms.clip(lists[0], 1.0)
+    with pytest.raises(dgn.DgnError):
+        norms.clip(lists[other], 1.0)
+    assert len(env.calls) == 1
+
+
+def test_calls_away_from_the_buffers_device_are_refused(monkeypatch):
+    """Kernels run on the current device's stream, which has to be that of the memory."""
+    env = Lists(monkeypatch)
+    a = values.AdamBuffers(*env.make())
+    a.step(**ADAM)
+    monkeypatch.setattr(values, "_current_device", lambda: 1)
+    with pytest.raises(dgn.DgnError):
+        a.step(**ADAM)
+    assert len(env.calls) == 1
