@@ -4,6 +4,7 @@ norms, clipping and update.  Allocation, checks of types and shapes, and marshal
 The library sees addresses; what a tensor's type, shape and strides say is checked here.  Every method raises
 ``DgnError`` for what is refused, by these checks or by the library.  Kernels run on the current stream, or on
 ``stream``; a caller who uses another stream than the one its tensors belong to orders the two, as for any kernel.
+Calls on one owner share its outputs and scratch: they must not overlap, whether from several streams or host threads.
 """
 from __future__ import annotations
 
@@ -54,6 +55,17 @@ def _dense(t, shape, dtype, index, where):
     return t.data_ptr()
 
 
+def _strides(d, **strides):
+    """The description ``d`` with these row strides: itself, if it has them, else another (a call may still read ``d``)."""
+    for name, value in strides.items():
+        if getattr(d, name) != value:
+            d = b.dgn_scan_desc.from_buffer_copy(d)
+            for name, value in strides.items():
+                setattr(d, name, value)
+            break
+    return d
+
+
 def _desc(tokens, seqs, channels, group, kind, dtype):
     _need(kind in GATES and dtype in DTYPES, "gate kind or element type")
     return b.dgn_scan_desc(num_tokens=tokens, num_seqs=seqs, num_channels=channels, gate_group=group,
@@ -88,17 +100,18 @@ class ScanBuffers:
             self.dh0 = new(num_seqs, num_channels, dtype=torch.float32)
 
     def _inputs(self, x, gate, seq_rowptr, h0):
-        d, at = self._d, self._index
-        px, d.x_stride = _rows(x, self._wide, self.dtype, at, "x")
-        pg, d.gate_stride = _rows(gate, self._gates, self.dtype, at, "gate")
+        at = self._index
+        px, sx = _rows(x, self._wide, self.dtype, at, "x")
+        pg, sg = _rows(gate, self._gates, self.dtype, at, "gate")
         pr = _dense(seq_rowptr, self._ptr, torch.int64, at, "seq_rowptr")
-        return px, pg, pr, _dense(h0, self._states, torch.float32, at, "h0")
+        return px, sx, pg, sg, pr, _dense(h0, self._states, torch.float32, at, "h0")
 
     def forward(self, x, gate, seq_rowptr, h0=None, stream=None):
         """``x`` [tokens, channels], ``gate`` [tokens, heads], ``seq_rowptr`` int64 [seqs + 1], ``h0`` float [seqs, channels]:
         may be ``final`` itself, for sequences that go on from call to call."""
-        px, pg, pr, ph = self._inputs(x, gate, seq_rowptr, h0)
-        b._check(b._lib.dgn_scan_forward(ctypes.byref(self._d), px, pg, pr, ph, self.y.data_ptr(), self.final.data_ptr(),
+        px, sx, pg, sg, pr, ph = self._inputs(x, gate, seq_rowptr, h0)
+        d = self._d = _strides(self._d, x_stride=sx, gate_stride=sg)
+        b._check(b._lib.dgn_scan_forward(ctypes.byref(d), px, pg, pr, ph, self.y.data_ptr(), self.final.data_ptr(),
                                          b._dp(self._carry), self._scratch.data_ptr(), self._scratch_bytes,
                                          _queue(self._index, stream)), "dgn_scan_forward")
 
@@ -106,12 +119,13 @@ class ScanBuffers:
         """Gradients for ``dy`` [tokens, channels] and ``dfinal`` float [seqs, channels] of the last ``forward``.  ``dfinal`` may be
         ``dh0``; ``h0`` may not be ``final``, where ``forward`` has written since."""
         _need(self.train, "backward of buffers made without train")
-        px, pg, pr, ph = self._inputs(x, gate, seq_rowptr, h0)
+        px, sx, pg, sg, pr, ph = self._inputs(x, gate, seq_rowptr, h0)
         if ph:
             _need(abs(ph - self.final.data_ptr()) >= 4 * self.num_seqs * self.num_channels, "h0 of backward: final has been written")
-        py, self._d.dy_stride = _rows(dy, self._wide, self.dtype, self._index, "dy")
+        py, sy = _rows(dy, self._wide, self.dtype, self._index, "dy")
+        d = self._d = _strides(self._d, x_stride=sx, gate_stride=sg, dy_stride=sy)
         pf = _dense(dfinal, self._states, torch.float32, self._index, "dfinal")
-        b._check(b._lib.dgn_scan_backward(ctypes.byref(self._d), px, pg, pr, ph, b._dp(self._carry), py, pf,
+        b._check(b._lib.dgn_scan_backward(ctypes.byref(d), px, pg, pr, ph, b._dp(self._carry), py, pf,
                                           self.dx.data_ptr(), self.dgate.data_ptr(), self.dh0.data_ptr(),
                                           self._scratch.data_ptr(), self._scratch_bytes, _queue(self._index, stream)),
                  "dgn_scan_backward")
@@ -134,9 +148,10 @@ class ScanStepBuffers:
     def step(self, x, gate, slots, state_in, state_out=None, stream=None):
         """Row r takes its state from row ``slots[r]`` of ``state_in`` (float [slots, channels]) and leaves it in the same
         row of ``state_out`` (default: ``state_in`` itself).  ``slots``: int32, -1 for an idle row, or None: row r."""
-        d, at = self._d, self._index
-        px, d.x_stride = _rows(x, self._wide, self.dtype, at, "x")
-        pg, d.gate_stride = _rows(gate, self._gates, self.dtype, at, "gate")
+        at = self._index
+        px, sx = _rows(x, self._wide, self.dtype, at, "x")
+        pg, sg = _rows(gate, self._gates, self.dtype, at, "gate")
+        d = self._d = _strides(self._d, x_stride=sx, gate_stride=sg)
         ps = _dense(slots, self._one, torch.int32, at, "slots")
         pi = _dense(state_in, self._pool, torch.float32, at, "state_in")
         po = pi if state_out is None else _dense(state_out, self._pool, torch.float32, at, "state_out")
@@ -180,19 +195,16 @@ class TensorList:
             self.close()
 
 
-def _fill_reach(r, lst, num_sets, mask, ids):
-    """``r``: the owner's own structure, filled for this call."""
-    r.num_sets = num_sets
+def _reach(lst, num_sets, mask, ids):
     if mask is None:
         _need(ids is None, "tensor_ids without tensor_mask")
-        r.tensor_mask, r.num_words, r.tensor_ids = None, 0, None
-        return
+        return b.dgn_reach(num_sets)
     at = lst.index
     if mask.dtype is not torch.int64 or mask.dim() != 1 or mask.get_device() != at or not mask.is_contiguous():
         raise b.DgnError(b.DGN_ERR_INVALID_ARG, "tensor_mask")
     # (a mask of no words has no address, which would say that there is no mask: the list's own is not read)
-    r.tensor_mask, r.num_words = mask.data_ptr() or lst._mem.data_ptr(), mask.numel()
-    r.tensor_ids = _dense(ids, (len(lst),), torch.int32, at, "tensor_ids")
+    return b.dgn_reach(num_sets, mask.data_ptr() or lst._mem.data_ptr(), mask.numel(),
+                       _dense(ids, (len(lst),), torch.int32, at, "tensor_ids"))
 
 
 class GradientBuffers:
@@ -208,22 +220,20 @@ class GradientBuffers:
         b._check(rc, "dgn_list_norms_workspace")
         self.norms = torch.empty(max(num_sets, 1), dtype=torch.float32, device=grads.device)
         self._scratch, self._scratch_bytes = torch.empty(sb, dtype=torch.uint8, device=grads.device), sb
-        self._reach = b.dgn_reach()
 
     def norm(self, mask=None, ids=None, stream=None):
         """Fills ``norms`` [num_sets]."""
-        r = self._reach
-        _fill_reach(r, self.grads, self.num_sets, mask, ids)
+        r = _reach(self.grads, self.num_sets, mask, ids)
         b._check(b._lib.dgn_list_norms(self.grads.handle, ctypes.byref(r), self.norms.data_ptr(), self._scratch.data_ptr(),
                                        self._scratch_bytes, _queue(self.grads.index, stream)), "dgn_list_norms")
 
     def clip(self, out: TensorList, max_norm, eps=1e-6, mask=None, ids=None, stream=None):
         """Writes the gradients, scaled so that no set's norm is above ``max_norm``, to ``out`` (may be the list itself);
         goes by ``norms`` as the last ``norm`` call left them."""
-        at, r = self.grads.index, self._reach
+        at = self.grads.index
         if out.index != at:
             raise b.DgnError(b.DGN_ERR_INVALID_ARG, "clip: a list of another device")
-        _fill_reach(r, self.grads, self.num_sets, mask, ids)
+        r = _reach(self.grads, self.num_sets, mask, ids)
         b._check(b._lib.dgn_list_clip(self.grads.handle, out.handle, ctypes.byref(r), self.norms.data_ptr(), max_norm, eps,
                                       _queue(at, stream)), "dgn_list_clip")
 
@@ -238,7 +248,6 @@ class AdamBuffers:
         self._need_open()
         _need(all(t.index == grads.index for t in self._all), "AdamBuffers: lists of several devices")
         self.grads = grads
-        self._reach = b.dgn_reach()
         self._lists = b.dgn_adam_lists(*(None if t is None else t.handle for t in (grads, params, m, v, out_params, out_m, out_v, copy)))
 
     def _need_open(self):       # (the library keeps nothing of a list that is closed, and takes none for `in place`)
@@ -253,8 +262,7 @@ class AdamBuffers:
             num_sets = norms.numel() if num_sets is None else num_sets
             _need(norms.dtype is torch.float32 and norms.is_contiguous() and norms.numel() >= num_sets
                   and norms.get_device() == self.grads.index, "norms")
-        r = self._reach
-        _fill_reach(r, self.grads, (64 if mask is not None else 1) if num_sets is None else num_sets, mask, ids)
+        r = _reach(self.grads, (64 if mask is not None else 1) if num_sets is None else num_sets, mask, ids)
         o = b.dgn_adam_options(lr, beta1, beta2, eps, weight_decay, step, int(skip_nonfinite), max_norm, clip_eps)
         b._check(b._lib.dgn_list_adam(ctypes.byref(self._lists), ctypes.byref(r), None if norms is None else norms.data_ptr(),
                                       ctypes.byref(o), _queue(self.grads.index, stream)), "dgn_list_adam")

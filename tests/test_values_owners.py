@@ -10,8 +10,7 @@ from paper_1707_08265_amd import values
 
 def test_a_mask_of_no_words_is_still_a_mask():
     lst = type("Two", (SimpleNamespace,), {"__len__": lambda self: 2})(index=-1, _mem=torch.zeros(64, dtype=torch.uint8))
-    r = dgn.dgn_reach()
-    values._fill_reach(r, lst, 1, torch.zeros(0, dtype=torch.int64), torch.zeros(2, dtype=torch.int32))
+    r = values._reach(lst, 1, torch.zeros(0, dtype=torch.int64), torch.zeros(2, dtype=torch.int32))
     assert r.num_words == 0 and r.tensor_mask and r.tensor_ids
 
 
@@ -67,7 +66,7 @@ def test_lists_of_another_device_are_refused(monkeypatch, other):
     with pytest.raises(dgn.DgnError):
         values.AdamBuffers(*lists)
     norms = values.GradientBuffers.__new__(values.GradientBuffers)
-    norms.grads, norms.num_sets, norms._reach, norms.norms = lists[0], 1, dgn.dgn_reach(), torch.zeros(1)
+    norms.grads, norms.num_sets, norms.norms = lists[0], 1, torch.zeros(1)
     norms.clip(lists[0], 1.0)
     with pytest.raises(dgn.DgnError):
         norms.clip(lists[other], 1.0)
@@ -83,3 +82,28 @@ def test_calls_away_from_the_buffers_device_are_refused(monkeypatch):
     with pytest.raises(dgn.DgnError):
         a.step(**ADAM)
     assert len(env.calls) == 1
+
+
+def test_a_call_keeps_the_strides_that_it_was_given(monkeypatch):
+    """The library reads a call's description without Python's lock: the next call must not write to it."""
+    with monkeypatch.context() as m:
+        m.setattr(values, "_need", lambda ok, where: None)                  # (owners of host buffers are refused)
+        s, t = dgn.ScanBuffers(20, 2, 12, kind="decay", train=True, device="cpu"), dgn.ScanStepBuffers(20, 2, 12, device="cpu")
+    seen = []
+    for name in ("dgn_scan_forward", "dgn_scan_backward", "dgn_scan_step"):
+        monkeypatch.setattr(values.b._lib, name, lambda d, *a: seen.append(d._obj) or 0)
+    monkeypatch.setattr(values, "_current_device", lambda: -1)
+    monkeypatch.setattr(values.b, "_raw_stream", lambda index: 0)
+    ptr, pool = torch.tensor([0, 7, 20]), torch.zeros(2, 12)
+    wide = torch.zeros(20, 40, dtype=torch.bfloat16)
+    want = []
+    for a, c, e in [(40, 40, 40), (12, 40, 40), (12, 12, 40), (12, 12, 12), (40, 12, 12)]:
+        cut = lambda step: wide[:, 3:15] if step == 40 else wide[:, 3:15].contiguous()  # noqa: E731
+        s.forward(cut(a), cut(c), ptr)
+        s.backward(cut(c), cut(a), ptr, cut(e))
+        t.step(cut(a), cut(e), None, pool)
+        want += [(a, c, None), (c, a, e), (a, e, None)]
+    got = [(d.x_stride, d.gate_stride, d.dy_stride) for d in seen]
+    assert len(got) == len(want)
+    for g, w in zip(got, want):
+        assert g[:2] == w[:2] and w[2] in (None, g[2])
