@@ -59,10 +59,10 @@ template <class T, int V> struct Pack {
     }
     template <bool kStream = false> __device__ __forceinline__ void store(S *p) const
     {
-        if (kBytes == 2) put<kStream>(reinterpret_cast<uint16_t *>(p), (uint16_t)w[0]);
-        else if (kBytes == 4) put<kStream>(reinterpret_cast<Word *>(p), (Word)w[0]);
-        else if (kBytes == 8) put<kStream>(reinterpret_cast<Pair *>(p), Pair{w[0], w[1 % kWords]});
-        else put<kStream>(reinterpret_cast<Quad4 *>(p), Quad4{w[0], w[1 % kWords], w[2 % kWords], w[3 % kWords]});
+        if (kBytes == 2) put<kStream, sizeof(S)>(p, (uint16_t)w[0]);
+        else if (kBytes == 4) put<kStream, sizeof(S)>(p, (Word)w[0]);
+        else if (kBytes == 8) put<kStream, sizeof(S)>(p, Pair{w[0], w[1 % kWords]});
+        else put<kStream, sizeof(S)>(p, Quad4{w[0], w[1 % kWords], w[2 % kWords], w[3 % kWords]});
     }
     __device__ __forceinline__ float get(int i) const
     {

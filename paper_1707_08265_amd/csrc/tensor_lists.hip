@@ -34,7 +34,7 @@ template <> struct Run<F32> {
     static constexpr int kN = 4;
     Quad32 w;
     __device__ __forceinline__ void load(const float *p) { w = *reinterpret_cast<const Quad32 *>(p); }
-    template <bool kStream> __device__ __forceinline__ void store(float *p) const { put<kStream>(reinterpret_cast<Quad32 *>(p), w); }
+    template <bool kStream> __device__ __forceinline__ void store(float *p) const { put<kStream, 4>(p, w); }
     __device__ __forceinline__ float get(int i) const { return __uint_as_float(w[i]); }
     __device__ __forceinline__ void scale(float f)
     {
@@ -47,7 +47,7 @@ template <class T> struct Run16 {
     static constexpr int kN = 8;
     Quad16 w;
     __device__ __forceinline__ void load(const S *p) { w = *reinterpret_cast<const Quad16 *>(p); }
-    template <bool kStream> __device__ __forceinline__ void store(S *p) const { put<kStream>(reinterpret_cast<Quad16 *>(p), w); }
+    template <bool kStream> __device__ __forceinline__ void store(S *p) const { put<kStream, 2>(p, w); }
     __device__ __forceinline__ float get(int i) const { return half_of<T>(w[i / 2], i % 2); }
     __device__ __forceinline__ void scale(float f)
     {
@@ -62,26 +62,26 @@ template <class T> struct Four;
 template <> struct Four<F32> {
     template <bool kStream> static __device__ __forceinline__ void load(const float *p, float (&f)[4])
     {
-        const Quad32 w = take<kStream>(reinterpret_cast<const Quad32 *>(p));
+        const Quad32 w = take<kStream, 4, Quad32>(p);
 #pragma unroll
         for (int i = 0; i < 4; i++) f[i] = __uint_as_float(w[i]);
     }
     template <bool kStream> static __device__ __forceinline__ void store(float *p, const float (&f)[4])
     {
-        put<kStream>(reinterpret_cast<Quad32 *>(p), Quad32{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])});
+        put<kStream, 4>(p, Quad32{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])});
     }
 };
 template <class T> struct Four16 {
     typedef typename T::Store S;
     template <bool kStream> static __device__ __forceinline__ void load(const S *p, float (&f)[4])
     {
-        const Pair16 w = take<kStream>(reinterpret_cast<const Pair16 *>(p));
+        const Pair16 w = take<kStream, 2, Pair16>(p);
 #pragma unroll
         for (int i = 0; i < 4; i++) f[i] = half_of<T>(w[i / 2], i % 2);
     }
     template <bool kStream> static __device__ __forceinline__ void store(S *p, const float (&f)[4])
     {
-        put<kStream>(reinterpret_cast<Pair16 *>(p), Pair16{two_halves<T>(f[0], f[1]), two_halves<T>(f[2], f[3])});
+        put<kStream, 2>(p, Pair16{two_halves<T>(f[0], f[1]), two_halves<T>(f[2], f[3])});
     }
 };
 template <> struct Four<F16> : Four16<F16> {};

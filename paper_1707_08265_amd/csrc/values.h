@@ -15,12 +15,19 @@ struct BF16 { typedef __bf16 Store; };
 
 inline int element_size(int32_t dtype) { return dtype == DGN_F32 ? 4 : 2; }
 
-// Past the caches where kStream (see kStreamBytes).
-template <bool kStream, class V> __device__ __forceinline__ V take(const V *p) { return kStream ? __builtin_nontemporal_load(p) : *p; }
-template <bool kStream, class V> __device__ __forceinline__ void put(V *p, V v)
+// Past the caches where kStream (see kStreamBytes).  kAlign: what the address is aligned to (a number, as a type's alignment does not pass
+// through a template).
+template <class V, int kAlign> struct Placed { typedef V At __attribute__((aligned(kAlign))); };
+template <bool kStream, int kAlign, class V> __device__ __forceinline__ V take(const void *p)
 {
-    if (kStream) __builtin_nontemporal_store(v, p);
-    else *p = v;
+    typedef typename Placed<V, kAlign>::At At;
+    return kStream ? __builtin_nontemporal_load(static_cast<const At *>(p)) : *static_cast<const At *>(p);
+}
+template <bool kStream, int kAlign, class V> __device__ __forceinline__ void put(void *p, V v)
+{
+    typedef typename Placed<V, kAlign>::At At;
+    if (kStream) __builtin_nontemporal_store(v, static_cast<At *>(p));
+    else *static_cast<At *>(p) = v;
 }
 // What lanes of a wave wrote to LDS is there for the others.
 __device__ __forceinline__ void wave_fence()
