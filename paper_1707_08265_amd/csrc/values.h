@@ -77,7 +77,7 @@ hipError_t launch_scan_step(int dtype, int kind, const StepArgs &a, hipStream_t 
 constexpr int kListChunk = 8192;    // elements of a chunk
 struct alignas(16) ListChunk { void *data; uint32_t entry, n_type; };    // its first element, the tensor it is of, elements * 4 + type
 static_assert(sizeof(ListChunk) == 16, "a chunk is one load");
-struct ListView { const ListChunk *chunk; int32_t chunks, most; size_t bytes; };      // most: elements of the largest chunk; bytes: of all
+struct ListView { const ListChunk *chunk; int32_t chunks; int64_t elements; size_t bytes; };
 
 struct Reach { const u64 *mask; int64_t words; const int32_t *ids; int32_t sets; };   // which sets reach an entry: see reach_of
 struct ClipArgs { Reach reach; const float *norms; float max_norm, eps; };

@@ -235,13 +235,13 @@ int dgn_list_build(const dgn_list_desc *d, void *list_mem, size_t list_bytes, dg
     l->all_f32 = true;
     for (int64_t i = 0; i < d->count; i++) {
         l->numel[i] = d->numel[i];
+        l->v.elements += d->numel[i];
         l->v.bytes += (size_t)d->numel[i] * element_size(d->dtype[i]);
         l->dtype[i] = d->dtype[i];
         l->all_f32 = l->all_f32 && d->dtype[i] == DGN_F32;
         for (int64_t at = 0; at < d->numel[i]; at += kListChunk) {
             const int64_t left = d->numel[i] - at, of = left < kListChunk ? left : kListChunk;
             chunk[n++] = ListChunk{static_cast<char *>(d->data[i]) + at * element_size(d->dtype[i]), (uint32_t)i, (uint32_t)(of * 4 + d->dtype[i])};
-            if (of > l->v.most) l->v.most = (int32_t)of;
         }
     }
     l->count = d->count;
