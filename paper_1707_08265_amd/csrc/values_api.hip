@@ -134,7 +134,7 @@ int dgn_scan_forward(const dgn_scan_desc *d, const void *x, const void *gate, co
     if (scratch_bytes < need) return DGN_ERR_WORKSPACE_TOO_SMALL;
     const size_t e = element_size(d->dtype);
     if (misaligned(x, e) || misaligned(gate, e) || misaligned(y, e) || misaligned(h0, 4) || misaligned(final, 4) ||
-        misaligned(seq_rowptr, 8) || misaligned(carry, 8) || misaligned(scratch, 8))
+        misaligned(seq_rowptr, 8) || misaligned(carry, 4) || misaligned(scratch, 8))
         return DGN_ERR_INVALID_ARG;
     ScanArgs a = scan_args(d);
     a.x = x;
@@ -163,7 +163,7 @@ int dgn_scan_backward(const dgn_scan_desc *d, const void *x, const void *gate, c
     if (scratch_bytes < need) return DGN_ERR_WORKSPACE_TOO_SMALL;
     const size_t e = element_size(d->dtype);
     if (misaligned(x, e) || misaligned(gate, e) || misaligned(dy, e) || misaligned(dx, e) || misaligned(dgate, e) ||
-        misaligned(h0, 4) || misaligned(dfinal, 4) || misaligned(dh0, 4) || misaligned(seq_rowptr, 8) || misaligned(carry, 8) ||
+        misaligned(h0, 4) || misaligned(dfinal, 4) || misaligned(dh0, 4) || misaligned(seq_rowptr, 8) || misaligned(carry, 4) ||
         misaligned(scratch, 8))
         return DGN_ERR_INVALID_ARG;
     ScanArgs a = scan_args(d);
