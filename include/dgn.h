@@ -469,8 +469,7 @@ typedef struct dgn_scan_desc {
     int64_t gate_group;      /* consecutive channels that share a gate: divides num_channels; 1 = each its own */
     int32_t dtype;           /* of x, gate, y and their gradients: DGN_F32 / DGN_F16 / DGN_BF16          */
     int32_t gate_kind;       /* DGN_GATE_DECAY or DGN_GATE_SIGMOID                                        */
-    /* elements from one row to the next, at least the row's width; 0 = rows without gaps.  dx and dgate must not
-     * have rows that overlap anything else */
+    /* elements from one row to the next, at least the row's width; 0 = rows without gaps */
     int64_t x_stride, gate_stride, y_stride, dy_stride, dx_stride, dgate_stride;
 } dgn_scan_desc;
 
@@ -481,8 +480,9 @@ int dgn_scan_workspace(const dgn_scan_desc *desc, size_t *scratch_bytes, size_t 
 /* x [num_tokens][num_channels], gate [num_tokens][num_channels / gate_group], h0 float [num_seqs][num_channels] or
  * NULL -> y [num_tokens][num_channels], final float [num_seqs][num_channels] or NULL (the state after the last token;
  * h0 of an empty sequence), carry: carry_bytes for dgn_scan_backward, or NULL.  All DEVICE, aligned to their
- * elements; scratch to 8 bytes.  y may not overlap x or gate.  final may be h0, or overlap it (sequences that go on from call
- * to call: h0 is then copied first; a backward pass needs the states that were there before). */
+ * elements; scratch to 8 bytes.  y and final may not overlap each other or an input (DGN_ERR_INVALID_ARG; rows may lie between
+ * another's, if they are as far apart), but final may be h0, or overlap it (sequences that go on from call to call: h0 is then
+ * copied first; a backward pass needs the states that were there before). */
 int dgn_scan_forward(const dgn_scan_desc *desc, const void *x, const void *gate, const int64_t *seq_rowptr,
                      const float *h0, void *y, float *final, void *carry, void *scratch, size_t scratch_bytes,
                      dgn_stream stream);
@@ -490,7 +490,8 @@ int dgn_scan_forward(const dgn_scan_desc *desc, const void *x, const void *gate,
 /* Gradients for dy [num_tokens][num_channels] and dfinal float [num_seqs][num_channels] (or NULL: zero): dx, dgate (a
  * shared gate's is the sum over its channels) and dh0 float (or NULL: not asked for).  x, gate, seq_rowptr and h0 as
  * dgn_scan_forward had them, carry as it left it.  The states are computed again from there in 32 bits, so y is not
- * needed.  dh0 may be dfinal, or overlap it (dfinal is then copied first).  The same inputs give the same bits. */
+ * needed.  The gradients may not overlap each other or an input (DGN_ERR_INVALID_ARG), but dh0 may be h0, and may be dfinal
+ * or overlap it (dfinal is then copied first).  The same inputs give the same bits. */
 int dgn_scan_backward(const dgn_scan_desc *desc, const void *x, const void *gate, const int64_t *seq_rowptr,
                       const float *h0, const void *carry, const void *dy, const float *dfinal, void *dx, void *dgate,
                       float *dh0, void *scratch, size_t scratch_bytes, dgn_stream stream);
@@ -498,7 +499,8 @@ int dgn_scan_backward(const dgn_scan_desc *desc, const void *x, const void *gate
 /* One token for each of desc->num_tokens rows (num_seqs is not looked at): row r's state is row slots[r] of state_in
  * [num_slots][num_channels] (float) and goes to the same row of state_out, which may be state_in.  slots: DEVICE int32,
  * or NULL: row r has slot r.  A row whose slot is outside 0..num_slots-1 (-1: an idle row of the batch) touches no
- * state and gets y = 0.  No two rows may have the same slot. */
+ * state and gets y = 0.  No two rows may have the same slot.  y may be x, and gate if its rows are as wide; nothing else may
+ * overlap what is written (DGN_ERR_INVALID_ARG). */
 int dgn_scan_step(const dgn_scan_desc *desc, int64_t num_slots, const void *x, const void *gate, const int32_t *slots,
                   const float *state_in, float *state_out, void *y, dgn_stream stream);
 

@@ -62,6 +62,29 @@ ScanArgs scan_args(const dgn_scan_desc *d)
     return a;
 }
 
+// Rows in memory, in bytes.  Two of them meet if they have a byte in common; rows of one buffer may lie between each other's (columns of
+// a wider matrix), if they are as far apart.
+struct Span { const void *at; int64_t rows, stride, width; };
+bool meet(Span a, Span b)
+{
+    if (!a.at || !b.at || a.rows <= 0 || b.rows <= 0 || a.width <= 0 || b.width <= 0) return false;
+    if (a.rows == 1) a.stride = b.rows == 1 ? a.width : b.stride;
+    if (b.rows == 1) b.stride = a.stride;
+    const uintptr_t pa = (uintptr_t)a.at, pb = (uintptr_t)b.at;
+    if (pa > pb) return meet(b, a);
+    const uint64_t apart = pb - pa;
+    if (apart >= (unsigned __int128)(a.rows - 1) * (uint64_t)a.stride + (uint64_t)a.width) return false;
+    if (a.stride != b.stride) return true;
+    const int64_t off = (int64_t)(apart % (uint64_t)a.stride);
+    return off < a.width || a.stride - off < b.width;
+}
+template <int N> bool meets(Span a, const Span (&others)[N])
+{
+    for (int i = 0; i < N; i++) if (meet(a, others[i])) return true;
+    return false;
+}
+Span dense(const void *p, int64_t rows, int64_t row_bytes) { return Span{p, rows, row_bytes, row_bytes}; }      // (no gaps)
+
 int check_reach(const dgn_reach *r, const dgn_list *l, Reach *out)
 {
     *out = Reach{nullptr, 0, nullptr, 1};
@@ -137,6 +160,10 @@ int dgn_scan_forward(const dgn_scan_desc *d, const void *x, const void *gate, co
         misaligned(seq_rowptr, 8) || misaligned(carry, 4) || misaligned(scratch, 8))
         return DGN_ERR_INVALID_ARG;
     ScanArgs a = scan_args(d);
+    const int64_t n = a.tokens, b = e, state = a.channels * 4;
+    const Span in[] = {{x, n, a.x_stride * b, a.channels * b}, {gate, n, a.gate_stride * b, a.heads * b}, dense(seq_rowptr, a.seqs + 1, 8)};
+    const Span out = {y, n, a.y_stride * b, a.channels * b}, last = dense(final, a.seqs, state);
+    if (meets(out, in) || meets(last, in) || meet(out, last) || meet(out, dense(h0, a.seqs, state))) return DGN_ERR_INVALID_ARG;
     a.x = x;
     a.gate = gate;
     a.rowptr = seq_rowptr;
@@ -167,6 +194,14 @@ int dgn_scan_backward(const dgn_scan_desc *d, const void *x, const void *gate, c
         misaligned(scratch, 8))
         return DGN_ERR_INVALID_ARG;
     ScanArgs a = scan_args(d);
+    const int64_t n = a.tokens, b = e, state = a.channels * 4;
+    const Span in[] = {{x, n, a.x_stride * b, a.channels * b}, {gate, n, a.gate_stride * b, a.heads * b}, dense(seq_rowptr, a.seqs + 1, 8),
+                       {dy, n, a.dy_stride * b, a.channels * b}};
+    const Span states[] = {dense(h0, a.seqs, state), dense(dfinal, a.seqs, state), dense(dh0, a.seqs, state)};
+    const Span wide = {dx, n, a.dx_stride * b, a.channels * b}, gates = {dgate, n, a.dgate_stride * b, a.heads * b};
+    if (meets(wide, in) || meets(gates, in) || meets(states[2], in) || meet(wide, gates) || meets(wide, states) || meets(gates, states) ||
+        (meet(states[2], states[0]) && dh0 != h0))              // (dh0 in h0's place: each state is read before it is written)
+        return DGN_ERR_INVALID_ARG;
     a.x = x;
     a.gate = gate;
     a.rowptr = seq_rowptr;
@@ -195,6 +230,14 @@ int dgn_scan_step(const dgn_scan_desc *d, int64_t num_slots, const void *x, cons
         misaligned(slots, 4))
         return DGN_ERR_INVALID_ARG;
     const ScanArgs s = scan_args(d);
+    const int64_t n = s.tokens, b = e, state = s.channels * 4;
+    const Span in[] = {{x, n, s.x_stride * b, s.channels * b}, {gate, n, s.gate_stride * b, s.heads * b}, dense(slots, n, 4)};
+    const Span out = {y, n, s.y_stride * b, s.channels * b}, from = dense(state_in, num_slots, state), to = dense(state_out, num_slots, state);
+    if (meets(to, in) || meet(out, to) || meet(out, from) || (meet(to, from) && state_in != state_out)) return DGN_ERR_INVALID_ARG;
+    for (int k = 0; k < 3; k++) {       // (each thread reads its elements of x and gate before it writes the same ones)
+        const bool same = k < 2 && in[k].at == y && in[k].width == out.width && (n == 1 || in[k].stride == out.stride);
+        if (meet(out, in[k]) && !same) return DGN_ERR_INVALID_ARG;
+    }
     const StepArgs a = {s.tokens, num_slots, s.channels, s.group, s.x_stride, s.gate_stride, s.y_stride, x, gate, slots, state_in,
                         state_out, y, 0};
     DGN_HIP(launch_scan_step(d->dtype, d->gate_kind, a, static_cast<hipStream_t>(stream)));
