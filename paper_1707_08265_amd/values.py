@@ -165,6 +165,7 @@ class TensorList:
     def __init__(self, tensors, stream=None):
         self.tensors = list(tensors)
         n = len(self.tensors)
+        _need(n == 0 or isinstance(self.tensors[0], torch.Tensor), "TensorList")
         dev = self.tensors[0].device if n else torch.device("cuda", torch.cuda.current_device())
         self.device, self.index = dev, dev.index if dev.type == "cuda" else -1
         for t in self.tensors:

@@ -107,3 +107,9 @@ def test_a_call_keeps_the_strides_that_it_was_given(monkeypatch):
     assert len(got) == len(want)
     for g, w in zip(got, want):
         assert g[:2] == w[:2] and w[2] in (None, g[2])
+
+
+@pytest.mark.parametrize("bad", [[64], [None], [[1.0]], [torch.zeros(3), 64]])
+def test_lists_of_what_is_no_tensor_are_refused(bad):
+    with pytest.raises(dgn.DgnError):
+        dgn.TensorList(bad)
