@@ -61,3 +61,17 @@ def test_a_mask_of_no_words_reaches_nothing(dgn):  # noqa: F811
     for call in (lambda: b.norm(empty), lambda: b.clip(lst, 1.0, mask=empty), lambda: a.step(**ADAM, mask=empty)):
         with pytest.raises(dgn.DgnError):
             call()
+
+
+def test_a_list_keeps_the_memory_whose_addresses_it_has(dgn):  # noqa: F811
+    """A tensor is given other memory after the list was made: what the list points to is not handed out to anybody else."""
+    size = 3 << 20
+    t = torch.nn.Parameter(torch.ones(size, device="cuda"))
+    was = t.data_ptr()
+    lst = dgn.TensorList([t])
+    t.data = torch.full((size,), 2.0, device="cuda")
+    others = [torch.zeros(size, device="cuda") for _ in range(4)]
+    assert was not in [o.data_ptr() for o in others] + [t.data_ptr()]
+    b = dgn.GradientBuffers(lst)
+    b.norm()
+    assert abs(float(b.norms[0]) - size ** 0.5) <= 2.0 ** -23 * size ** 0.5       # the old memory's, as it says
