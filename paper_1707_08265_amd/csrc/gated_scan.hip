@@ -11,7 +11,7 @@
 // The rows, whatever sequences they belong to, are cut into strips; a wave takes a strip of 64 V channels.  What a strip does to the state
 // that comes into it is h -> A h + B (A the product of its gates, B its end from a state of zero), or h -> B if a sequence begins in it.
 // Three launches: the strips' (A, B); the states between strips, a short scan per channel; the strips again, now with the state that comes
-// into each (two launches for up to 512 rows, one for up to 128).  Nothing waits for anything within a launch, and the order of all sums
+// into each (two launches for up to 32 strips, one for up to 8).  Nothing waits for anything within a launch, and the order of all sums
 // is given by the sizes alone.  It is bound by memory: forward every element of x and gate is read twice, of gate and dy backward.
 // (In one launch, that reads x and gate once, a workgroup keeps its rows in registers until the workgroups before it have handed their state
 // on.  All of them then load, wait and store at the same time: 65 301 x 2 048 forward in f16 253 us, 10 000 x 1 000 43 us, training step of
@@ -779,7 +779,9 @@ static int elements_of(int dtype, const ScanArgs &a)
 // Rows of a strip: as few as give kStrips strips, which is what the card has waves for, and at least so many that a channel has no
 // more strips than the second launch keeps in registers -- from kKeep to kMostRows.
 constexpr int64_t kStrips = 8192, kChannelStrips = 1024;
-constexpr int64_t kFewStrips = 32;      // up to here a strip applies the links before it itself: 257 x 512 forward 14.6 us instead of 16.6
+// Up to so many strips each applies the links before it itself, without the launch between: 512 x 512 forward (32 strips) 12.9 us, with it
+// 14.0; 768 x 512 (48) 14.4 and 14.0.
+constexpr int64_t kFewStrips = 32;
 struct Layout { int V; Cut cut; int64_t rows, strips; size_t words, states, partial, before, bytes; };
 static Layout lay_out(int dtype, const ScanArgs &a)
 {
@@ -884,17 +886,14 @@ template <class T, int kKind> static hipError_t go(int dtype, bool back, ScanArg
     return hipGetLastError();
 }
 
-#define DGN_BY_TYPE(call)                                                                                     \
-    do {                                                                                                      \
-        if (dtype == DGN_F32) { typedef F32 T; if (kind == kDecay) call(T, kDecay); else call(T, kSigmoid); } \
-        else if (dtype == DGN_F16) { typedef F16 T; if (kind == kDecay) call(T, kDecay); else call(T, kSigmoid); } \
-        else { typedef BF16 T; if (kind == kDecay) call(T, kDecay); else call(T, kSigmoid); }                 \
-    } while (0)
+#define DGN_BY_KIND(T)                     \
+    if (kind == kDecay) DGN_GO(T, kDecay); \
+    else DGN_GO(T, kSigmoid)
 
 hipError_t launch_scan(int dtype, int kind, bool back, const ScanArgs &a, void *scratch, hipStream_t s)
 {
 #define DGN_GO(T, K) return go<T, K>(dtype, back, a, scratch, s)
-    DGN_BY_TYPE(DGN_GO);
+    DGN_BY_DTYPE(dtype, DGN_BY_KIND);
 #undef DGN_GO
 }
 
@@ -915,7 +914,7 @@ template <class T, int kKind> static void go_step(StepArgs a, hipStream_t s)
 hipError_t launch_scan_step(int dtype, int kind, const StepArgs &a, hipStream_t s)
 {
 #define DGN_GO(T, K) go_step<T, K>(a, s)
-    DGN_BY_TYPE(DGN_GO);
+    DGN_BY_DTYPE(dtype, DGN_BY_KIND);
 #undef DGN_GO
     return hipGetLastError();
 }

@@ -89,12 +89,6 @@ template <> struct Four<BF16> : Four16<BF16> {};
 
 __device__ __forceinline__ int elements(const ListChunk &c) { return (int)(c.n_type >> 2); }
 __device__ __forceinline__ int type(const ListChunk &c) { return (int)(c.n_type & 3); }
-#define DGN_BY_DTYPE(dtype, call)                 \
-    do {                                          \
-        if ((dtype) == DGN_F32) { call(F32); }    \
-        else if ((dtype) == DGN_F16) { call(F16); } \
-        else { call(BF16); }                      \
-    } while (0)
 
 // The sets that reach an entry: its word of the mask, or that of the tensor that it stands for (none, if there is no such
 // tensor); without a mask every set does.

@@ -14,6 +14,13 @@ struct F16 { typedef _Float16 Store; };
 struct BF16 { typedef __bf16 Store; };
 
 inline int element_size(int32_t dtype) { return dtype == DGN_F32 ? 4 : 2; }
+// call(T) for the element type.
+#define DGN_BY_DTYPE(dtype, call)                 \
+    do {                                          \
+        if ((dtype) == DGN_F32) { call(F32); }    \
+        else if ((dtype) == DGN_F16) { call(F16); } \
+        else { call(BF16); }                      \
+    } while (0)
 
 // Past the caches where kStream (see kStreamBytes).  kAlign: what the address is aligned to (a number, as a type's alignment does not pass
 // through a template).
