@@ -443,7 +443,8 @@ int dgn_selftest_wave_ops(void *buffer, size_t bytes, dgn_stream stream);
 /* ---- values of tensors: what a pruned training step runs next ------------------------------------- */
 
 /* These calls only enqueue: none waits, copies to the host or allocates (dgn_list_build does), so they can be
- * captured into a HIP graph. */
+ * captured into a HIP graph.  Numbers that a call is given by value are the captured call's at every replay: a captured
+ * dgn_list_adam applies one step's rates and bias corrections each time, and is to be captured anew (or called) where they change. */
 
 /* Element types.  Whatever the type, arithmetic is in 32 bits or more and a result is rounded once, when it is
  * stored (to nearest, ties to even). */
@@ -456,8 +457,9 @@ enum { DGN_F32 = 0, DGN_F16 = 1, DGN_BF16 = 2 };
  *      DGN_GATE_SIGMOID:  a_t = 1 / (1 + exp(-gate_t)) u_t = (1 - a_t) x_t
  * The state is held in 32 bits.  Sequences are rows of one [num_tokens] list one after the other: sequence q has the
  * rows seq_rowptr[q] .. seq_rowptr[q+1] - 1 (DEVICE int64 [num_seqs+1], ascending, within 0..num_tokens; any may be
- * empty).  Rows before the first and after the last sequence are neither read nor written, so buffers may have room
- * for more tokens than a batch has.  The lengths are never asked for on the host.  Row pointers that do not ascend
+ * empty).  Rows before the first and after the last sequence are not written and what they hold does not matter, so
+ * buffers may have room for more tokens than a batch has (they are gone over like the others: a call takes the time of
+ * num_tokens rows).  The lengths are never asked for on the host.  Row pointers that do not ascend
  * give unspecified values; rows outside 0..num_tokens are not touched.
  * A state that is no finite number stays none in its own sequence and channel and reaches no other.  Products of up to
  * 64 gates of a channel are formed and have to be in the range of floats, as they are for decays of magnitude up to 1.

@@ -390,8 +390,8 @@ __global__ __launch_bounds__(kStripWaves *kWave, 8) void k_scan_links(ScanArgs a
 
 // Second launch: the state that comes into each strip, states[strip][slot].  A workgroup has kSlots slots; the strips are cut into kPieces
 // pieces, each is put together, the pieces' links are applied one after the other, and each is gone through again: with its words in
-// registers where they are few (kEach > 0: at most so many), so that they are asked for once and all at once: 625 strips of 1 024 slots 6.5
-// instead of 8.3 us.  (With 32 of them, for 1 025 strips, 16.7 us instead of 10.2: too many registers for 1 024 threads.)
+// registers where they are few (kEach > 0: at most so many), so that they are asked for once and all at once: 625 strips of 1 024 slots 6.9
+// instead of 8.7 us.  (With 32 of them, for 1 025 strips, 21 us instead of 11: too many registers for 1 024 threads.)
 // A piece has any number of gates.  Products that only fall may reach 0; where one of the strips' is above 1, their product could pass the range
 // of floats though no state does (200 decays of 2, then 200 of 1/2): it is then held as a 64-bit fraction with an exponent beside it, and
 // applied in 64 bits.  (In 64 bits always: 3 us more.)
@@ -666,7 +666,7 @@ __device__ __forceinline__ void strip_gradients(const ScanArgs &a, const Strip<V
     }
 }
 
-// Third launch, backward: 65 537 x 1 024 in bf16, 688 MB in 137 us, 5.0 TB/s.  Four waves to a SIMD: with five or six, and registers spilled,
+// Third launch, backward: 65 537 x 1 024 in bf16, 688 MB in 141 us, 4.9 TB/s.  Four waves to a SIMD: with five or six, and registers spilled,
 // the training step took 409 and 474 us instead of 335.
 template <class T, int kKind, int V, bool kShared, bool kStream>
 __global__ __launch_bounds__(kStripWaves *kWave, 4) void k_scan_gradients(ScanArgs a)

@@ -263,7 +263,8 @@ class AdamBuffers:
 
     def step(self, lr, beta1, beta2, eps, weight_decay, step, norms=None, max_norm=1.0, clip_eps=1e-6, mask=None, ids=None,
              num_sets=None, skip_nonfinite=False, stream=None):
-        """``norms`` (of ``GradientBuffers``): gradients are scaled as ``clip`` would; ``num_sets`` defaults to their number."""
+        """``norms`` (of ``GradientBuffers``): gradients are scaled as ``clip`` would; ``num_sets`` defaults to their number.
+        Captured into a graph, every replay applies these rates and the bias corrections of this ``step``."""
         self._need_open()
         if norms is not None:
             num_sets = norms.numel() if num_sets is None else num_sets
