@@ -566,6 +566,117 @@ typedef struct dgn_adam_options {
 int dgn_list_adam(const dgn_adam_lists *lists, const dgn_reach *reach, const float *norms,
                   const dgn_adam_options *options, dgn_stream stream);
 
+/* ---- a selective recurrent layer: convolution, scan, and the way back to the residual -------------- */
+
+/* Like dgn_scan_*: only enqueue, rows are a list of sequences one after the other, 32-bit arithmetic, one rounding at the end;
+ * parameters, states of the scan and gradients of parameters are floats.  Rows that belong to no sequence are not written and
+ * what they hold does not matter.  Unless a call says otherwise, nothing that is written may overlap anything else that it is given
+ * (DGN_ERR_INVALID_ARG).  The same inputs give the same bits. */
+
+/* Short causal convolution, channel by channel, over the rows of ragged sequences:
+ *      p_t = bias + sum_j weight[j] x_{t - (num_taps - 1) + j},     y_t = p_t or p_t / (1 + exp(-p_t))
+ * Rows before a sequence's first are those of its state, the num_taps - 1 rows before it, oldest first (zero without one).
+ * dtype: of x, y, states and the gradients of these; weight float [num_channels][num_taps], bias float [num_channels] or NULL. */
+enum { DGN_ACT_NONE = 0, DGN_ACT_SILU = 1 };
+typedef struct dgn_conv_desc {
+    int64_t num_tokens, num_seqs, num_channels;
+    int32_t num_taps;        /* 2..4 */
+    int32_t activation;      /* DGN_ACT_NONE or DGN_ACT_SILU */
+    int32_t dtype, reserved;
+    int64_t x_stride, y_stride, dy_stride, dx_stride;    /* elements from row to row; 0 = rows without gaps */
+} dgn_conv_desc;
+
+/* Bytes of scratch for dgn_conv_forward / dgn_conv_backward (the larger); may be NULL. */
+int dgn_conv_workspace(const dgn_conv_desc *desc, size_t *scratch_bytes);
+
+/* x [num_tokens][num_channels], state0 [num_seqs][num_taps - 1][num_channels] or NULL -> y like x, final like state0 or NULL: the last
+ * num_taps - 1 rows of each sequence, with its state in front (state0 itself for an empty one).  final may be state0 or overlap it (it is
+ * copied first).  All DEVICE, aligned to their elements; scratch to 8 bytes. */
+int dgn_conv_forward(const dgn_conv_desc *desc, const void *x, const float *weight, const float *bias, const int64_t *seq_rowptr,
+                     const void *state0, void *y, void *final, void *scratch, size_t scratch_bytes, dgn_stream stream);
+
+/* Gradients for dy (like y) and dfinal (like final, or NULL: zero): dx, dweight, dbias (or NULL: not asked for), dstate0 (or NULL).  Nothing of
+ * the forward pass is kept, p is computed again. */
+int dgn_conv_backward(const dgn_conv_desc *desc, const void *x, const float *weight, const float *bias, const int64_t *seq_rowptr,
+                      const void *state0, const void *dy, const void *dfinal, void *dx, float *dweight, float *dbias, void *dstate0,
+                      void *scratch, size_t scratch_bytes, dgn_stream stream);
+
+/* One token for each of desc->num_tokens rows (num_seqs is not looked at): row r's state is row slots[r] of state_in
+ * [num_slots][num_taps - 1][num_channels] and goes, moved on by one row, to the same row of state_out, which may be state_in.  slots as for
+ * dgn_scan_step: NULL is row r, a slot outside 0..num_slots-1 touches no state and gets y = 0, no two rows have the same.  y may be x. */
+int dgn_conv_step(const dgn_conv_desc *desc, int64_t num_slots, const void *x, const float *weight, const float *bias,
+                  const int32_t *slots, const void *state_in, void *state_out, void *y, dgn_stream stream);
+
+/* Selective scan: num_states states for each channel, whose decay and input depend on the token.  Per sequence and channel c of group g
+ * (num_channels / num_groups neighbouring channels share B and C):
+ *      d = log(1 + exp(delta_t[c] + delta_bias[c]))
+ *      h_t[n] = exp(d A[c][n]) h_{t-1}[n] + d x_t[c] B_t[g][n],        h_{-1} = h0 (zero without one)
+ *      y_t[c] = sum_n C_t[g][n] h_t[n] + D[c] x_t[c],   times z_t[c] / (1 + exp(-z_t[c])) with z
+ * States are floats.  A is at most 0 in use; exp(A times the sum of up to 64 rows' d) is formed and has to be in the range of floats.  A state
+ * that is no finite number stays none in its own sequence and channel and reaches no other (but a channel's y and gradients are sums over
+ * its states, those of B and C over the channels of a group). */
+typedef struct dgn_select_desc {
+    int64_t num_tokens, num_seqs, num_channels;
+    int64_t num_states;      /* 1..256 */
+    int64_t num_groups;      /* divides num_channels */
+    int32_t dtype, reserved; /* of x, delta, B, C, z, y and their gradients */
+    /* elements from row to row; 0 = rows without gaps */
+    int64_t x_stride, delta_stride, b_stride, c_stride, z_stride, y_stride;
+    int64_t dy_stride, dx_stride, ddelta_stride, db_stride, dc_stride, dz_stride;
+} dgn_select_desc;
+
+typedef struct dgn_select_inputs {
+    const void *x, *delta;           /* [num_tokens][num_channels]                          */
+    const float *A;                  /* [num_channels][num_states]                          */
+    const void *B, *C;               /* [num_tokens][num_groups * num_states]               */
+    const float *D, *delta_bias;     /* [num_channels], or NULL: zero                       */
+    const void *z;                   /* like x, or NULL: no outer gate                      */
+    const int64_t *seq_rowptr;       /* [num_seqs + 1], as for dgn_scan_forward             */
+    const float *h0;                 /* [num_seqs][num_channels][num_states], or NULL: zero */
+} dgn_select_inputs;
+
+typedef struct dgn_select_grads {
+    void *dx, *ddelta;
+    float *dA;
+    void *dB, *dC;
+    float *dD, *ddelta_bias;         /* or NULL: not asked for */
+    void *dz;                        /* with z */
+    float *dh0;                      /* or NULL */
+} dgn_select_grads;
+
+/* Bytes of scratch for dgn_select_forward / dgn_select_backward (the larger), and of the states that a forward pass keeps for the backward
+ * pass.  Either pointer may be NULL. */
+int dgn_select_workspace(const dgn_select_desc *desc, size_t *scratch_bytes, size_t *carry_bytes);
+
+/* -> y [num_tokens][num_channels], final like h0 or NULL (the state after the last token; h0 of an empty sequence; may be h0 or overlap it),
+ * carry: carry_bytes for dgn_select_backward, or NULL.  All DEVICE, aligned to their elements; scratch and carry to 16 bytes. */
+int dgn_select_forward(const dgn_select_desc *desc, const dgn_select_inputs *in, void *y, float *final, void *carry, void *scratch,
+                       size_t scratch_bytes, dgn_stream stream);
+
+/* Gradients for dy (like y) and dfinal float (like final, or NULL: zero).  The inputs as dgn_select_forward had them, carry as it left it. */
+int dgn_select_backward(const dgn_select_desc *desc, const dgn_select_inputs *in, const void *carry, const void *dy, const float *dfinal,
+                        const dgn_select_grads *out, void *scratch, size_t scratch_bytes, dgn_stream stream);
+
+/* One token for each of desc->num_tokens rows (num_seqs, seq_rowptr and h0 are not looked at), on states in a pool
+ * [num_slots][num_channels][num_states]; slots as for dgn_conv_step; state_out may be state_in, y may be x, delta or z. */
+int dgn_select_step(const dgn_select_desc *desc, int64_t num_slots, const dgn_select_inputs *in, const int32_t *slots,
+                    const float *state_in, float *state_out, void *y, dgn_stream stream);
+
+/* Dropout added to a residual:  y = residual + keep x / (1 - rate),  the mask from a counter and never stored:
+ * the gradient for dy is the same call with dy for x and without a residual.
+ * Element e = row * num_columns + column is dropped where its 16-bit draw is below round(65536 rate), and what is kept is scaled by the inverse of
+ * the share that this keeps.  Draw e is half e % 2 (low first) of word e / 2 % 4 of the block e / 8: Philox 4x32 with ten
+ * rounds, key key[0], counter (e / 8, key[1]), each as two words, low first.  key: DEVICE uint64 [2], read when the call runs: add 1
+ * to key[1] between steps, also between replays of a captured graph.  What x holds in dropped places does not matter.  y may be x
+ * or the residual, rows where they are. */
+typedef struct dgn_dropout_desc {
+    int64_t num_rows, num_columns;
+    int32_t dtype, reserved;
+    double rate;             /* 0..1 */
+    int64_t x_stride, residual_stride, y_stride;         /* elements from row to row; 0 = rows without gaps */
+} dgn_dropout_desc;
+int dgn_dropout(const dgn_dropout_desc *desc, const void *x, const void *residual, const uint64_t *key, void *y, dgn_stream stream);
+
 /* ---- misc ---------------------------------------------------------------------------------- */
 const char *dgn_strerror(int code);
 int dgn_version(void);

@@ -9,3 +9,4 @@ from .binding import (DeviceGraph, PruneBuffers, BackwardPruneBuffers, InplaceBu
                       DgnError, EXPORTS,
                       LIB_PATH)  # noqa: F401
 from .values import AdamBuffers, GradientBuffers, ScanBuffers, ScanStepBuffers, TensorList  # noqa: F401
+from .layers import ConvBuffers, ConvStepBuffers, DropoutBuffers, SelectiveBuffers, SelectiveStepBuffers  # noqa: F401

@@ -29,6 +29,7 @@ DGN_ERR_BAD_CSR = -9
 
 DGN_F32, DGN_F16, DGN_BF16 = 0, 1, 2
 DGN_GATE_DECAY, DGN_GATE_SIGMOID = 0, 1
+DGN_ACT_NONE, DGN_ACT_SILU = 0, 1
 
 EXPORTS = [
     "dgn_graph_build_workspace", "dgn_graph_build", "dgn_graph_from_csr_workspace", "dgn_graph_from_csr",
@@ -39,6 +40,8 @@ EXPORTS = [
     "dgn_scan_workspace", "dgn_scan_forward", "dgn_scan_backward", "dgn_scan_step",
     "dgn_list_workspace", "dgn_list_build", "dgn_list_destroy", "dgn_list_norms_workspace", "dgn_list_norms",
     "dgn_list_clip", "dgn_list_adam",
+    "dgn_conv_workspace", "dgn_conv_forward", "dgn_conv_backward", "dgn_conv_step",
+    "dgn_select_workspace", "dgn_select_forward", "dgn_select_backward", "dgn_select_step", "dgn_dropout",
     "dgn_version",
     "dgn_last_hip_error",
 ]
@@ -106,6 +109,32 @@ class dgn_adam_options(ctypes.Structure):
                 ("max_norm", ctypes.c_float), ("clip_eps", ctypes.c_float)]
 
 
+class dgn_conv_desc(ctypes.Structure):
+    _fields_ = [("num_tokens", c_int64), ("num_seqs", c_int64), ("num_channels", c_int64), ("num_taps", c_int32),
+                ("activation", c_int32), ("dtype", c_int32), ("reserved", c_int32), ("x_stride", c_int64), ("y_stride", c_int64),
+                ("dy_stride", c_int64), ("dx_stride", c_int64)]
+
+
+class dgn_select_desc(ctypes.Structure):
+    _fields_ = [(n, c_int64) for n in ("num_tokens", "num_seqs", "num_channels", "num_states", "num_groups")] + [
+        ("dtype", c_int32), ("reserved", c_int32)] + [(n, c_int64) for n in (
+            "x_stride", "delta_stride", "b_stride", "c_stride", "z_stride", "y_stride", "dy_stride", "dx_stride",
+            "ddelta_stride", "db_stride", "dc_stride", "dz_stride")]
+
+
+class dgn_select_inputs(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in ("x", "delta", "A", "B", "C", "D", "delta_bias", "z", "seq_rowptr", "h0")]
+
+
+class dgn_select_grads(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in ("dx", "ddelta", "dA", "dB", "dC", "dD", "ddelta_bias", "dz", "dh0")]
+
+
+class dgn_dropout_desc(ctypes.Structure):
+    _fields_ = [("num_rows", c_int64), ("num_columns", c_int64), ("dtype", c_int32), ("reserved", c_int32),
+                ("rate", ctypes.c_double), ("x_stride", c_int64), ("residual_stride", c_int64), ("y_stride", c_int64)]
+
+
 PHASES = ["clear", "seed", "traverse", "count", "scan", "scatter", "total"]
 
 
@@ -158,6 +187,16 @@ def _load() -> ctypes.CDLL:
     lib.dgn_scan_forward.argtypes = [POINTER(dgn_scan_desc)] + [c_void_p] * 8 + [c_size_t, c_void_p]
     lib.dgn_scan_backward.argtypes = [POINTER(dgn_scan_desc)] + [c_void_p] * 11 + [c_size_t, c_void_p]
     lib.dgn_scan_step.argtypes = [POINTER(dgn_scan_desc), c_int64] + [c_void_p] * 7
+    lib.dgn_conv_workspace.argtypes = [POINTER(dgn_conv_desc), POINTER(c_size_t)]
+    lib.dgn_conv_forward.argtypes = [POINTER(dgn_conv_desc)] + [c_void_p] * 8 + [c_size_t, c_void_p]
+    lib.dgn_conv_backward.argtypes = [POINTER(dgn_conv_desc)] + [c_void_p] * 12 + [c_size_t, c_void_p]
+    lib.dgn_conv_step.argtypes = [POINTER(dgn_conv_desc), c_int64] + [c_void_p] * 8
+    lib.dgn_select_workspace.argtypes = [POINTER(dgn_select_desc), POINTER(c_size_t), POINTER(c_size_t)]
+    lib.dgn_select_forward.argtypes = [POINTER(dgn_select_desc), POINTER(dgn_select_inputs)] + [c_void_p] * 4 + [c_size_t, c_void_p]
+    lib.dgn_select_backward.argtypes = [POINTER(dgn_select_desc), POINTER(dgn_select_inputs)] + [c_void_p] * 3 + [
+        POINTER(dgn_select_grads), c_void_p, c_size_t, c_void_p]
+    lib.dgn_select_step.argtypes = [POINTER(dgn_select_desc), c_int64, POINTER(dgn_select_inputs)] + [c_void_p] * 5
+    lib.dgn_dropout.argtypes = [POINTER(dgn_dropout_desc)] + [c_void_p] * 5
     lib.dgn_list_workspace.argtypes = [POINTER(dgn_list_desc), POINTER(c_size_t)]
     lib.dgn_list_build.argtypes = [POINTER(dgn_list_desc), c_void_p, c_size_t, c_void_p, POINTER(c_void_p)]
     lib.dgn_list_destroy.argtypes = [c_void_p]
@@ -448,6 +487,55 @@ def dgn_scan_backward(desc, x, gate, seq_rowptr, h0, carry, dy, dfinal, dx, dgat
 def dgn_scan_step(desc, num_slots, x, gate, slots, state_in, state_out, y, stream=None) -> int:
     return _lib.dgn_scan_step(_ref(desc), num_slots, _dp(x), _dp(gate), _dp(slots), _dp(state_in), _dp(state_out), _dp(y),
                               _stream(stream))
+
+
+def dgn_conv_workspace(desc):
+    """Returns (rc, scratch bytes)."""
+    n = c_size_t(0)
+    rc = _lib.dgn_conv_workspace(_ref(desc), ctypes.byref(n))
+    return rc, n.value
+
+
+def dgn_conv_forward(desc, x, weight, bias, seq_rowptr, state0, y, final, scratch, scratch_bytes, stream=None) -> int:
+    return _lib.dgn_conv_forward(_ref(desc), _dp(x), _dp(weight), _dp(bias), _dp(seq_rowptr), _dp(state0), _dp(y), _dp(final),
+                                 _dp(scratch), scratch_bytes, _stream(stream))
+
+
+def dgn_conv_backward(desc, x, weight, bias, seq_rowptr, state0, dy, dfinal, dx, dweight, dbias, dstate0, scratch, scratch_bytes,
+                      stream=None) -> int:
+    return _lib.dgn_conv_backward(_ref(desc), _dp(x), _dp(weight), _dp(bias), _dp(seq_rowptr), _dp(state0), _dp(dy), _dp(dfinal),
+                                  _dp(dx), _dp(dweight), _dp(dbias), _dp(dstate0), _dp(scratch), scratch_bytes, _stream(stream))
+
+
+def dgn_conv_step(desc, num_slots, x, weight, bias, slots, state_in, state_out, y, stream=None) -> int:
+    return _lib.dgn_conv_step(_ref(desc), num_slots, _dp(x), _dp(weight), _dp(bias), _dp(slots), _dp(state_in), _dp(state_out),
+                              _dp(y), _stream(stream))
+
+
+def dgn_select_workspace(desc):
+    """Returns (rc, scratch bytes, bytes of the states kept for the backward pass)."""
+    s, c = c_size_t(0), c_size_t(0)
+    rc = _lib.dgn_select_workspace(_ref(desc), ctypes.byref(s), ctypes.byref(c))
+    return rc, s.value, c.value
+
+
+def dgn_select_forward(desc, inputs, y, final, carry, scratch, scratch_bytes, stream=None) -> int:
+    return _lib.dgn_select_forward(_ref(desc), _ref(inputs), _dp(y), _dp(final), _dp(carry), _dp(scratch), scratch_bytes,
+                                   _stream(stream))
+
+
+def dgn_select_backward(desc, inputs, carry, dy, dfinal, grads, scratch, scratch_bytes, stream=None) -> int:
+    return _lib.dgn_select_backward(_ref(desc), _ref(inputs), _dp(carry), _dp(dy), _dp(dfinal), _ref(grads), _dp(scratch),
+                                    scratch_bytes, _stream(stream))
+
+
+def dgn_select_step(desc, num_slots, inputs, slots, state_in, state_out, y, stream=None) -> int:
+    return _lib.dgn_select_step(_ref(desc), num_slots, _ref(inputs), _dp(slots), _dp(state_in), _dp(state_out), _dp(y),
+                                _stream(stream))
+
+
+def dgn_dropout(desc, x, residual, key, y, stream=None) -> int:
+    return _lib.dgn_dropout(_ref(desc), _dp(x), _dp(residual), _dp(key), _dp(y), _stream(stream))
 
 
 def dgn_list_workspace(desc):

@@ -16,9 +16,7 @@
 // (In one launch, that reads x and gate once, a workgroup keeps its rows in registers until the workgroups before it have handed their state
 // on.  All of them then load, wait and store at the same time: 65 301 x 2 048 forward in f16 253 us, 10 000 x 1 000 43 us, training step of
 // 65 537 x 1 024 500 us.)
-#include "values.h"
-
-#include <type_traits>
+#include "rows.h"
 
 namespace dgn {
 
@@ -39,63 +37,6 @@ template <class T, int kKind> __device__ __forceinline__ void open_gate(float g,
     a = g < 0.0f ? er : r;                  // (NaN: r is NaN)
     b = g < 0.0f ? r : er;
 }
-
-__device__ __forceinline__ int64_t row_bound(int64_t v, int64_t tokens) { return v < 0 ? 0 : v > tokens ? tokens : v; }
-
-__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
-
-typedef uint32_t Word __attribute__((aligned(2)));
-typedef uint32_t Pair __attribute__((ext_vector_type(2), aligned(2)));
-typedef uint32_t Quad4 __attribute__((ext_vector_type(4), aligned(4)));
-
-// V neighbouring elements, at an address that is aligned to one, as they are in memory.
-template <class T, int V> struct Pack {
-    typedef typename T::Store S;
-    static constexpr int kBytes = V * (int)sizeof(S), kWords = kBytes < 4 ? 1 : kBytes / 4;
-    uint32_t w[kWords];
-    __device__ __forceinline__ void load(const S *p)
-    {
-        if (kBytes == 2) w[0] = *reinterpret_cast<const uint16_t *>(p);
-        else if (kBytes == 4) w[0] = *reinterpret_cast<const Word *>(p);
-        else if (kBytes == 8) { const Pair v = *reinterpret_cast<const Pair *>(p); w[0] = v[0]; w[1 % kWords] = v[1]; }
-        else {
-            const Quad4 v = *reinterpret_cast<const Quad4 *>(p);
-#pragma unroll
-            for (int i = 0; i < 4; i++) w[i % kWords] = v[i];
-        }
-    }
-    template <bool kStream = false> __device__ __forceinline__ void store(S *p) const
-    {
-        if (kBytes == 2) put<kStream, sizeof(S)>(p, (uint16_t)w[0]);
-        else if (kBytes == 4) put<kStream, sizeof(S)>(p, (Word)w[0]);
-        else if (kBytes == 8) put<kStream, sizeof(S)>(p, Pair{w[0], w[1 % kWords]});
-        else put<kStream, sizeof(S)>(p, Quad4{w[0], w[1 % kWords], w[2 % kWords], w[3 % kWords]});
-    }
-    __device__ __forceinline__ float get(int i) const
-    {
-        if (sizeof(S) == 4) return __uint_as_float(w[i]);
-        const uint16_t h = (uint16_t)(w[i / 2 % kWords] >> (i % 2 * 16));
-        return (float)__builtin_bit_cast(typename std::conditional<sizeof(S) == 2, S, _Float16>::type, h);
-    }
-    __device__ __forceinline__ void set(const float (&f)[V])
-    {
-        if (sizeof(S) == 4) {
-#pragma unroll
-            for (int i = 0; i < V; i++) w[i % kWords] = __float_as_uint(f[i]);
-        } else {
-            typedef typename std::conditional<sizeof(S) == 2, S, _Float16>::type H;
-            typedef H H2 __attribute__((ext_vector_type(2)));
-#pragma unroll
-            for (int i = 0; i < V; i += 2) w[i / 2 % kWords] = __builtin_bit_cast(uint32_t, H2{(H)f[i], (H)f[i + 1 < V ? i + 1 : i]});
-        }
-    }
-    // From here on the compiler knows nothing of the value.
-    __device__ __forceinline__ void forget()
-    {
-#pragma unroll
-        for (int i = 0; i < kWords; i++) asm volatile("" : "+v"(w[i]));
-    }
-};
 
 // What a run of rows does to the state that comes into it: A h + B, or B alone if `cut` (a sequence begins in it, or for gradients ends).
 // In memory: B in the low half, A in the high one (an A that is no number as the usual one, and as another to say `cut`).
@@ -126,15 +67,6 @@ inline Cut cut_channels(int64_t channels, int64_t group, int V)
     const int64_t parts = (group + room - 1) / room;
     return Cut{channels / group * parts, (int32_t)room, (int32_t)parts};
 }
-__device__ __forceinline__ int64_t uniform(int64_t v)
-{
-    return (int64_t)((u64)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
-}
-__device__ __forceinline__ int64_t divide(int64_t n, int64_t by)       // (both fit 32 bits but in the largest of calls)
-{
-    return n >> 32 || by >> 32 ? n / by : (int64_t)((uint32_t)n / (uint32_t)by);
-}
-
 // First channel of a block, how many it has, and which part of its head it is.
 struct Block { int64_t c; int32_t width, part; };
 __device__ __forceinline__ Block block_of(const ScanArgs &a, int64_t block)
@@ -155,21 +87,6 @@ constexpr int kStripWaves = 4;          // waves of a workgroup; each has a stri
 struct Marks {
     int32_t begin[kMostRows], end[kMostRows];       // the sequence whose first / last row this is, or -1
 };
-// Number of rowptr[0 .. n-1] below `value`; one wave, 64 looks at a time.
-__device__ __forceinline__ int64_t rows_below(const int64_t *rowptr, int64_t n, int64_t value)
-{
-    int64_t l = 0, r = n;
-    while (l < r) {
-        const int64_t step = (r - l + kWave - 1) / kWave, at = l + lane_id() * step;
-        const int below = __popcll(__ballot(at < r && rowptr[at < r ? at : l] < value));
-        if (below == 0) return l;
-        const int64_t top = l + below * step;
-        l += (below - 1) * step + 1;
-        r = top < r ? top : r;
-    }
-    return l;
-}
-
 // A lane's V states of a row that is the same for the wave (nothing: zero).
 template <int V> __device__ __forceinline__ void load_state(const float *row, uint32_t mine, float (&h)[V])
 {

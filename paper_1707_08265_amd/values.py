@@ -59,7 +59,7 @@ def _strides(d, **strides):
     """The description ``d`` with these row strides: itself, if it has them, else another (a call may still read ``d``)."""
     for name, value in strides.items():
         if getattr(d, name) != value:
-            d = b.dgn_scan_desc.from_buffer_copy(d)
+            d = type(d).from_buffer_copy(d)
             for name, value in strides.items():
                 setattr(d, name, value)
             break
