@@ -113,29 +113,16 @@ template <class T, int V> __device__ __forceinline__ void conv_store(void *base,
     p.store(static_cast<typename T::Store *>(base) + at);
 }
 
-// Sequences without rows: out = in (or zero), by the workgroups from `first` on.
-template <class T> __device__ __forceinline__ void copy_empties(const ConvArgs &a, const void *in, void *out, int64_t wave, int64_t waves)
-{
-    typedef typename T::Store S;
-    const int64_t width = (int64_t)(a.taps - 1) * a.channels;
-    for (int64_t q0 = wave * kWave; q0 < a.seqs; q0 += waves * kWave) {
-        const int64_t q = q0 + lane_id();
-        const bool empty = q < a.seqs && row_bound(a.rowptr[q], a.tokens) >= row_bound(a.rowptr[q + 1], a.tokens);
-        for (u64 some = __ballot(empty); some; some &= some - 1) {
-            const int64_t at = (q0 + __builtin_ctzll(some)) * width;
-            for (int64_t i = lane_id(); i < width; i += kWave)
-                static_cast<S *>(out)[at + i] = in ? static_cast<const S *>(in)[at + i] : (S)0.0f;
-        }
-    }
-}
-
 template <class T, int V, int K, bool kSilu>
 __global__ __launch_bounds__(kConvWaves *kWave) void k_conv_forward(ConvArgs a)
 {
     __shared__ int32_t s_own[kConvWaves][kWave];
     const int64_t groups = (a.runs + kConvWaves - 1) / kConvWaves;
     if (blockIdx.x >= groups * a.blocks) {
-        if (a.final) copy_empties<T>(a, a.state0, a.final, (blockIdx.x - groups * a.blocks) * kConvWaves + wave_id(), (gridDim.x - groups * a.blocks) * kConvWaves);
+        typedef typename T::Store S;
+        if (a.final)
+            copy_empties(a.rowptr, a.seqs, a.tokens, (K - 1) * a.channels, static_cast<const S *>(a.state0), static_cast<S *>(a.final),
+                         (blockIdx.x - groups * a.blocks) * kConvWaves + wave_id(), (gridDim.x - groups * a.blocks) * kConvWaves);
         return;
     }
     const int64_t group = divide(blockIdx.x, a.blocks), block = blockIdx.x - group * a.blocks;
@@ -176,7 +163,9 @@ __global__ __launch_bounds__(kConvWaves *kWave) void k_conv_backward(ConvArgs a)
     __shared__ float s_sum[kConvWaves][K + 1][V][kWave];
     const int64_t groups = (a.runs + kConvWaves - 1) / kConvWaves;
     if (blockIdx.x >= groups * a.blocks) {
-        if (a.dstate0) copy_empties<T>(a, a.dfinal, a.dstate0, (blockIdx.x - groups * a.blocks) * kConvWaves + wave_id(), (gridDim.x - groups * a.blocks) * kConvWaves);
+        if (a.dstate0)
+            copy_empties(a.rowptr, a.seqs, a.tokens, (K - 1) * a.channels, static_cast<const S *>(a.dfinal), static_cast<S *>(a.dstate0),
+                         (blockIdx.x - groups * a.blocks) * kConvWaves + wave_id(), (gridDim.x - groups * a.blocks) * kConvWaves);
         return;
     }
     const int64_t group = divide(blockIdx.x, a.blocks), block = blockIdx.x - group * a.blocks;
@@ -374,19 +363,20 @@ static ConvLayout conv_layout(int dtype, const ConvArgs &a)
 bool conv_fits(int dtype, const ConvArgs &a)        // launches of less than 2^32 threads
 {
     const ConvLayout l = conv_layout(dtype, a);
-    return l.groups * l.blocks < ((int64_t)1 << 24) - 64 && a.channels < ((int64_t)1 << 28);
+    return l.groups * l.blocks < ((int64_t)1 << 24) - 1024 && a.channels < ((int64_t)1 << 28);
 }
 size_t conv_scratch_bytes(int dtype, const ConvArgs &a) { return conv_layout(dtype, a).bytes; }
 
 template <class T, int V, int K, bool kSilu> static void go_conv(bool back, const ConvArgs &a, const ConvLayout &l, hipStream_t s)
 {
-    const int64_t empties = (a.seqs + kWave * kConvWaves - 1) / (kWave * kConvWaves);
-    const dim3 grid((unsigned)(l.groups * l.blocks + (empties < 64 ? empties : 64))), threads(kConvWaves * kWave);
+    const int64_t empties = (back ? a.dstate0 : a.final) ? copy_groups(a.seqs, (K - 1) * a.channels, kConvWaves) : 0;
+    const dim3 grid((unsigned)(l.groups * l.blocks + empties)), threads(kConvWaves * kWave);
+    const bool any = grid.x > 0;
     if (!back) {
-        hipLaunchKernelGGL((k_conv_forward<T, V, K, kSilu>), grid, threads, 0, s, a);
+        if (any) hipLaunchKernelGGL((k_conv_forward<T, V, K, kSilu>), grid, threads, 0, s, a);
         return;
     }
-    if (a.seqs > 0) hipLaunchKernelGGL((k_conv_backward<T, V, K, kSilu>), grid, threads, 0, s, a);
+    if (a.seqs > 0 && any) hipLaunchKernelGGL((k_conv_backward<T, V, K, kSilu>), grid, threads, 0, s, a);
     const dim3 sums((unsigned)((a.channels + kWave - 1) / kWave), (unsigned)(a.taps + 1));
     hipLaunchKernelGGL(k_conv_sums, sums, dim3(kSumWaves * kWave), 0, s, a, a.seqs > 0 ? l.groups : 0);
 }

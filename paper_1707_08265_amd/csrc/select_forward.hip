@@ -1,0 +1,349 @@
+// Selective scan over ragged sequences: the forward pass, the states between strips, and one token (see select.h).
+#include "select.h"
+
+namespace dgn {
+
+// First launch: what a strip does to the state that comes into it.
+template <class T, int S, int L>
+__global__ __launch_bounds__(kSelectWaves *kWave) void k_select_ends(SelectArgs a)
+{
+    typedef Lane<S, L> Mine;
+    __shared__ int32_t s_own[kSelectWaves][kWave];
+    __shared__ __attribute__((aligned(16))) float s_b[kSelectWaves][kSelectBatch * Mine::kWide];
+    float *lds = s_b[wave_id()];
+    Mine ln;
+    if (!ln.find(a, (int64_t)blockIdx.x * kSelectWaves + wave_id())) return;
+    ln.mark(a, s_own[wave_id()]);
+    if (lane_id() == 0) a.cuts[ln.strip] = ln.begin != 0;       // (the same from every wave of the strip)
+    if (!((ln.valid & ~ln.end) >> (ln.rows - 1) & 1)) {         // (nothing goes on past it; without a beginning no row belongs to a sequence)
+        const float none[S] = {};
+        ln.store_own(a.ends + ln.own(a, ln.strip), none);
+        if (ln.active && ln.part == 0) a.spans[ln.strip * a.channels + ln.c] = 0.0f;
+        return;
+    }
+    const int from = ln.begin ? 63 - __builtin_clzll(ln.begin) : 0;
+    float A2[S], h[S], span = 0.0f;
+    ln.decays(a, A2);
+#pragma unroll
+    for (int i = 0; i < S; i++) h[i] = 0.0f;
+    if (ln.begin) ln.load(a, a.h0, ln.q(from), h);
+    const float bias = a.delta_bias ? a.delta_bias[ln.c] : 0.0f;
+    Column<T, kSelectBatch> x, delta;
+    Shared<T, Mine::kWide, kSelectBatch> B;
+    const auto fetch = [&](int k0) {
+        x.load(a.x, a.x_stride, ln.row0 + k0, ln.c, a.tokens);
+        delta.load(a.delta, a.delta_stride, ln.row0 + k0, ln.c, a.tokens);
+        B.load(a.B, a.b_stride, ln.row0 + k0, a, ln.group);
+    };
+    fetch(from);
+    for (int k0 = from; k0 < ln.rows; k0 += kSelectBatch) {
+        wave_fence();
+        B.put(lds);
+        wave_fence();
+        const Column<T, kSelectBatch> x1 = x, d1 = delta;
+        if (k0 + kSelectBatch < ln.rows) fetch(k0 + kSelectBatch);
+        const auto rows = [&](auto some) {
+#pragma unroll
+            for (int k = 0; k < kSelectBatch; k++) {
+                if (some.value && k0 + k >= ln.rows) break;
+                const float d = step_of(d1.get(k) + bias), u = d * x1.get(k);
+                float b[S];
+                take_states(lds + k * Mine::kWide + ln.n0, b);
+#pragma unroll
+                for (int i = 0; i < S; i++) h[i] = fmaf(exp2_of(d * A2[i]), h[i], u * b[i]);
+                span += d;
+            }
+        };
+        if (k0 + kSelectBatch <= ln.rows) rows(std::false_type());
+        else rows(std::true_type());
+    }
+    ln.store_own(a.ends + ln.own(a, ln.strip), h);
+    if (ln.active && ln.part == 0) a.spans[ln.strip * a.channels + ln.c] = span;
+}
+
+// Second launch: the state that comes into each strip.  A workgroup has 64 states (a wave reads 64 neighbours of a strip) and kPieces pieces of
+// the strips: each is put together, the pieces before are applied one after the other, and each is gone through again.
+constexpr int kPieces = 16;
+__global__ __launch_bounds__(kPieces *kWave) void k_select_states(SelectArgs a, int wide, bool back)
+{
+    __shared__ float s_end[kPieces][kWave], s_span[kPieces][kWave];
+    __shared__ bool s_cut[kPieces];
+    const int64_t slots = a.channels * wide, slot = (int64_t)blockIdx.x * kWave + lane_id(), at = slot < slots ? slot : slots - 1;
+    const int64_t c = divide(at, wide), n = at - c * wide;
+    const float A2 = n < a.states ? a.A[c * a.states + n] * kLog2e : 0.0f;
+    const int piece = wave_id();
+    const int64_t each = (a.strips + kPieces - 1) / kPieces, from = piece * each, to = from + each < a.strips ? from + each : a.strips;
+    float h = 0.0f, span = 0.0f;
+    bool cut = false;
+    float *out = back ? a.back : a.before;
+    const auto every = [&](auto write) {
+#pragma unroll 4
+        for (int64_t k = from; k < to; k++) {
+            const int64_t strip = back ? a.strips - 1 - k : k;
+            const float e = a.ends[strip * slots + at], d = a.spans[strip * a.channels + c];
+            const bool here = a.cuts[strip];
+            if (write.value) { if (slot < slots) out[strip * slots + slot] = h; }
+            h = here ? e : fmaf(exp2_of(d * A2), h, e);
+            span += d;
+            cut = cut || here;
+        }
+    };
+    every(std::false_type());
+    s_end[piece][lane_id()] = h;
+    s_span[piece][lane_id()] = span;
+    if (lane_id() == 0) s_cut[piece] = cut;
+    __syncthreads();
+    h = 0.0f;
+    for (int p = 0; p < piece; p++) {
+        const float e = s_end[p][lane_id()];
+        h = s_cut[p] ? e : fmaf(exp2_of(s_span[p][lane_id()] * A2), h, e);
+    }
+    every(std::true_type());
+}
+void select_states(const SelectArgs &a, int wide, bool back, hipStream_t s)
+{
+    const int64_t groups = (a.channels * wide + kWave - 1) / kWave;
+    hipLaunchKernelGGL(k_select_states, dim3((unsigned)groups), dim3(kPieces * kWave), 0, s, a, wide, back);
+}
+
+// Third launch.
+template <class T, int S, int L>
+__global__ __launch_bounds__(kSelectWaves *kWave) void k_select_outputs(SelectArgs a)
+{
+    typedef Lane<S, L> Mine;
+    typedef typename T::Store E;
+    __shared__ int32_t s_own[kSelectWaves][kWave];
+    __shared__ __attribute__((aligned(16))) float s_bc[kSelectWaves][2][kSelectBatch * Mine::kWide];
+    const int64_t number = (int64_t)blockIdx.x * kSelectWaves + wave_id(), strips = (a.strips * a.blocks + kSelectWaves - 1) / kSelectWaves;
+    if (blockIdx.x >= strips) {
+        if (a.final)
+            copy_empties(a.rowptr, a.seqs, a.tokens, a.channels * a.states, a.h0, a.final, number - strips * kSelectWaves, (gridDim.x - strips) * kSelectWaves);
+        return;
+    }
+    float (&lds)[2][kSelectBatch * Mine::kWide] = s_bc[wave_id()];
+    Mine ln;
+    if (!ln.find(a, number)) return;
+    float A2[S], h[S];
+    ln.decays(a, A2);
+    ln.template before<false>(a, A2, h);
+    const float bias = a.delta_bias ? a.delta_bias[ln.c] : 0.0f, D = a.D ? a.D[ln.c] : 0.0f;
+    Column<T, kSelectBatch> x, delta, z;
+    Shared<T, Mine::kWide, kSelectBatch> B, C;
+    const auto fetch = [&](int k0) {
+        x.load(a.x, a.x_stride, ln.row0 + k0, ln.c, a.tokens);
+        delta.load(a.delta, a.delta_stride, ln.row0 + k0, ln.c, a.tokens);
+        if (a.z) z.load(a.z, a.z_stride, ln.row0 + k0, ln.c, a.tokens);
+        B.load(a.B, a.b_stride, ln.row0 + k0, a, ln.group);
+        C.load(a.C, a.c_stride, ln.row0 + k0, a, ln.group);
+    };
+    fetch(0);
+    ln.mark(a, s_own[wave_id()]);                               // (with the first rows on their way)
+    for (int k0 = 0; k0 < ln.rows; k0 += kSelectBatch) {
+        wave_fence();
+        B.put(lds[0]);
+        C.put(lds[1]);
+        wave_fence();
+        const Column<T, kSelectBatch> x1 = x, d1 = delta, z1 = z;
+        if (k0 + kSelectBatch < ln.rows) fetch(k0 + kSelectBatch);
+        if (a.kept && k0 % kSelectKeep == 0) ln.store_own(a.kept + ln.own(a, (ln.row0 + k0) / kSelectKeep), h);
+        const uint32_t valid = ln.valid >> k0 & 0xff, begin = ln.begin >> k0 & 0xff, end = ln.end >> k0 & 0xff;
+        E *to = static_cast<E *>(a.y) + (ln.row0 + k0) * a.y_stride + ln.c;
+        const auto rows = [&](auto some) {
+#pragma unroll
+            for (int k = 0; k < kSelectBatch; k++) {
+                if (some.value && !(valid >> k & 1)) continue;
+                const float d = step_of(d1.get(k) + bias), u = d * x1.get(k);
+                if (some.value && (begin >> k & 1)) ln.load(a, a.h0, ln.q(k0 + k), h);
+                float b[S], c[S], y = 0.0f;
+                take_states(lds[0] + k * Mine::kWide + ln.n0, b);
+                take_states(lds[1] + k * Mine::kWide + ln.n0, c);
+#pragma unroll
+                for (int i = 0; i < S; i++) {
+                    h[i] = fmaf(exp2_of(d * A2[i]), h[i], u * b[i]);
+                    y = fmaf(c[i], h[i], y);
+                }
+                y = sum_channel<L>(y);
+                if (a.D) y = fmaf(D, x1.get(k), y);
+                if (a.z) y *= z1.get(k) * gate_of<T>(z1.get(k));
+                if (ln.active && ln.part == 0) to[k * a.y_stride] = (E)y;
+                if (some.value && (end >> k & 1) && a.final) ln.store(a, a.final, ln.q(k0 + k), h);
+            }
+        };
+        // (most rows are in the middle of a sequence)
+        if (valid == 0xff && (begin | end) == 0) rows(std::false_type());
+        else rows(std::true_type());
+    }
+}
+
+template <class T, int S, int L> static void go_forward(const SelectArgs &a, hipStream_t s)
+{
+    const int64_t groups = (a.strips * a.blocks + kSelectWaves - 1) / kSelectWaves;
+    const int64_t empties = a.final ? copy_groups(a.seqs, a.channels * a.states, kSelectWaves) : 0;
+    const dim3 threads(kSelectWaves * kWave);
+    if (a.strips > 1) {
+        hipLaunchKernelGGL((k_select_ends<T, S, L>), dim3((unsigned)groups), threads, 0, s, a);
+        if (a.before) select_states(a, S * L, false, s);
+    }
+    if (groups + empties > 0) hipLaunchKernelGGL((k_select_outputs<T, S, L>), dim3((unsigned)(groups + empties)), threads, 0, s, a);
+}
+void select_forward(int dtype, const SelectArgs &a, const SelectLayout &l, hipStream_t s)
+{
+#define DGN_CALL(S, L) go_forward<Type, S, L>(a, s)
+#define DGN_GO(T)                                   \
+    do {                                            \
+        typedef T Type;                             \
+        DGN_BY_LANES(l.S, l.L, DGN_CALL);           \
+    } while (0)
+    DGN_BY_DTYPE(dtype, DGN_GO);
+#undef DGN_GO
+#undef DGN_CALL
+}
+
+// One token for each row: lanes as above, of a row's channel block.
+template <class T, int L>
+__global__ __launch_bounds__(256) void k_select_step(SelectStepArgs s)
+{
+    constexpr int S = 4;
+    typedef typename T::Store E;
+    const SelectArgs &a = s.in;
+    for (int64_t number = (int64_t)blockIdx.x * 4 + wave_id(); number < a.tokens * a.blocks; number += (int64_t)gridDim.x * 4) {
+        const int64_t row = divide(number, a.blocks), slot = s.slot ? s.slot[row] : row;
+        Lane<S, L> ln;
+        ln.place(a, number - row * a.blocks);
+        float y = 0.0f;
+        if (slot >= 0 && slot < s.slots) {
+            float A2[S], h[S];
+            ln.load(a, s.state_in, slot, h);
+            ln.decays(a, A2);
+            const float d = step_of((float)static_cast<const E *>(a.delta)[row * a.delta_stride + ln.c] + (a.delta_bias ? a.delta_bias[ln.c] : 0.0f));
+            const float x = (float)static_cast<const E *>(a.x)[row * a.x_stride + ln.c], u = d * x;
+            const E *b = static_cast<const E *>(a.B) + row * a.b_stride + ln.group * a.states + ln.n0,
+                    *c = static_cast<const E *>(a.C) + row * a.c_stride + ln.group * a.states + ln.n0;
+#pragma unroll
+            for (int i = 0; i < S; i++) {
+                const float bi = i < ln.count ? (float)b[i] : 0.0f, ci = i < ln.count ? (float)c[i] : 0.0f;
+                h[i] = fmaf(exp2_of(d * A2[i]), h[i], u * bi);
+                y = fmaf(ci, h[i], y);
+            }
+            ln.store(a, s.state_out, slot, h);
+            y = sum_channel<L>(y);
+            if (a.D) y = fmaf(a.D[ln.c], x, y);
+            if (a.z) {
+                const float z = (float)static_cast<const E *>(a.z)[row * a.z_stride + ln.c];
+                y *= z * gate_of<T>(z);
+            }
+        }
+        if (ln.active && ln.part == 0) static_cast<E *>(a.y)[row * a.y_stride + ln.c] = (E)y;
+    }
+}
+
+// Lanes: 16 states each where that gives enough waves, else four.  Rows of a strip: as few as give kSelectStrips waves, from kSelectKeep to
+// kSelectMostRows.
+constexpr int64_t kSelectStrips = 8192, kManyWaves = 2048;
+SelectLayout select_layout(const SelectArgs &a)
+{
+    SelectLayout l;
+    l.wide = 4;
+    while (l.wide < a.states) l.wide *= 2;
+    const int64_t share = a.channels / a.groups;
+    const auto blocks = [&](int S) { const int64_t width = kWave / (l.wide / S); return (share + width - 1) / width; };
+    const int64_t back = l.wide <= 16 ? 64 : 1024 / l.wide;             // channels of a workgroup of the backward pass
+    l.back_group_blocks = (share + back - 1) / back;
+    l.back_blocks = l.back_group_blocks * a.groups;
+    l.S = l.wide >= 16 && blocks(16) * a.groups * ((a.tokens + kSelectKeep - 1) / kSelectKeep) >= kManyWaves ? 16 : 4;
+    l.L = l.wide / l.S;
+    l.group_blocks = blocks(l.S);
+    l.blocks = l.group_blocks * a.groups;
+    l.rows = a.tokens * l.blocks / kSelectStrips / kSelectKeep * kSelectKeep;
+    l.rows = l.rows < kSelectKeep ? kSelectKeep : l.rows > kSelectMostRows ? kSelectMostRows : l.rows;
+    l.strips = (a.tokens + l.rows - 1) / l.rows;
+    const size_t state = (size_t)a.channels * l.wide * sizeof(float), chunks = (size_t)((a.tokens + kSelectKeep - 1) / kSelectKeep);
+    const auto room = [](size_t v) { return (v + 255) / 256 * 256; };
+    l.carry = chunks * state;
+    l.ends = 0;
+    l.before = l.ends + room(l.strips * state);
+    l.spans = l.before + room(l.strips * state);
+    l.cuts = l.spans + room((size_t)l.strips * a.channels * sizeof(float));
+    l.partial = l.cuts + room((size_t)l.strips * sizeof(int32_t));
+    l.copy = l.partial;             // (the one forward, the other backward)
+    l.shared = l.partial + room(l.strips * (state + 2 * a.channels * sizeof(float)));
+    const size_t copied = l.copy + (size_t)a.seqs * a.channels * a.states * sizeof(float),
+                 sums = l.shared + (size_t)l.back_group_blocks * a.tokens * a.groups * 2 * l.wide * sizeof(float);
+    l.bytes = copied > sums ? copied : sums;
+    return l;
+}
+bool select_fits(int, const SelectArgs &a)          // launches of less than 2^32 threads
+{
+    const SelectLayout l = select_layout(a);
+    const int64_t most = l.blocks > l.back_blocks ? l.blocks : l.back_blocks;
+    return l.strips * most < ((int64_t)1 << 25) && a.channels * l.wide < ((int64_t)1 << 27);
+}
+size_t select_scratch_bytes(int, const SelectArgs &a) { return select_layout(a).bytes; }
+size_t select_carry_bytes(int, const SelectArgs &a) { return select_layout(a).carry; }
+
+__global__ __launch_bounds__(256) void k_copy_floats(const float *from, float *to, int64_t n)
+{
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) to[i] = from[i];
+}
+
+hipError_t launch_select(int dtype, bool back, const SelectArgs &args, void *carry, void *scratch, hipStream_t s)
+{
+    const SelectLayout l = select_layout(args);
+    SelectArgs a = args;
+    char *mem = static_cast<char *>(scratch);
+    const auto at = [&](size_t v) { return reinterpret_cast<float *>(mem + v); };
+    a.strips = l.strips;
+    a.blocks = back ? l.back_blocks : l.blocks;
+    a.group_blocks = (int32_t)(back ? l.back_group_blocks : l.group_blocks);
+    a.rows = (int32_t)l.rows;
+    a.ends = at(l.ends);
+    a.spans = at(l.spans);
+    a.cuts = reinterpret_cast<int32_t *>(mem + l.cuts);
+    a.before = a.back = l.strips > kFewStrips ? at(l.before) : nullptr;
+    a.kept = static_cast<float *>(carry);
+    a.partial = at(l.partial);
+    a.shared = at(l.shared);
+    if (back) {
+        select_backward(dtype, a, l, s);
+        return hipGetLastError();
+    }
+    const int64_t n = a.seqs * a.channels * a.states;
+    if (a.h0 && a.final && a.h0 < a.final + n && a.final < a.h0 + n) {      // (strips read and write states in any order)
+        const int64_t groups = (n + 255) / 256;
+        hipLaunchKernelGGL(k_copy_floats, dim3((unsigned)(groups < 4096 ? groups : 4096)), dim3(256), 0, s, a.h0, at(l.copy), n);
+        a.h0 = at(l.copy);
+    }
+    select_forward(dtype, a, l, s);
+    return hipGetLastError();
+}
+
+hipError_t launch_select_step(int dtype, const SelectStepArgs &args, hipStream_t s)
+{
+    const SelectLayout l = select_layout(args.in);
+    SelectStepArgs a = args;
+    const int64_t width = kWave / (l.wide / 4), share = a.in.channels / a.in.groups;
+    a.in.group_blocks = (int32_t)((share + width - 1) / width);
+    a.in.blocks = a.in.group_blocks * a.in.groups;
+    const int64_t n = (a.in.tokens * a.in.blocks + 3) / 4;
+    const dim3 grid((unsigned)(n < (1 << 22) ? n : 1 << 22)), threads(256);
+#define DGN_CALL(S, L) hipLaunchKernelGGL((k_select_step<Type, L>), grid, threads, 0, s, a)
+#define DGN_GO(T)                                   \
+    do {                                            \
+        typedef T Type;                             \
+        switch (l.wide / 4) {                       \
+        case 1: DGN_CALL(4, 1); break;              \
+        case 2: DGN_CALL(4, 2); break;              \
+        case 4: DGN_CALL(4, 4); break;              \
+        case 8: DGN_CALL(4, 8); break;              \
+        case 16: DGN_CALL(4, 16); break;            \
+        case 32: DGN_CALL(4, 32); break;            \
+        default: DGN_CALL(4, 64);                   \
+        }                                           \
+    } while (0)
+    DGN_BY_DTYPE(dtype, DGN_GO);
+#undef DGN_GO
+#undef DGN_CALL
+    return hipGetLastError();
+}
+
+}  // namespace dgn

@@ -6,10 +6,10 @@ import pytest
 
 from paper_1707_08265_amd import build as lib_build
 
-OWN = ("causal_conv.hip", "selective_scan.hip", "dropout.hip", "gated_scan.hip", "rows.h", "layer.h", "values.h")
+OWN = ("causal_conv.hip", "select_forward.hip", "select_backward.hip", "dropout.hip", "gated_scan.hip", "select.h", "rows.h", "layer.h", "values.h")
 
 
-@pytest.mark.parametrize("source", OWN[:4])
+@pytest.mark.parametrize("source", OWN[:5])
 def test_no_access_assumes_more_than_its_element(source):
     r = subprocess.run(["hipcc", *lib_build.FLAGS, "-fsyntax-only", os.path.join(lib_build.CSRC, source)], capture_output=True,
                        text=True, timeout=300)
