@@ -115,27 +115,33 @@ __device__ __forceinline__ RowSeq sequences_of(const int64_t *rowptr, int64_t se
     return r;
 }
 
-// States of sequences without rows, `width` elements each: out = in (or zero).  A unit is kCopySlice elements of 64 sequences'; one after the
-// other they are taken by the waves of the launch that are left for it.
-constexpr int64_t kCopySlice = 1024;
+// States of sequences without rows, `width` elements each: out = in (or zero).  A unit is kCopySlice elements of every kCopyPhases-th of those
+// among 64 sequences; one after the other they are taken by the waves of the launch that are left for it.  (in may be out: what is read first
+// goes to registers, so that the reads do not wait for the writes.)
+constexpr int64_t kCopySlice = 1024, kCopyPhases = 8;
 inline int64_t copy_groups(int64_t seqs, int64_t width, int waves)     // workgroups of so many waves
 {
-    const int64_t units = (seqs + kWave - 1) / kWave * ((width + kCopySlice - 1) / kCopySlice), n = (units + waves - 1) / waves;
+    const int64_t units = (seqs + kWave - 1) / kWave * kCopyPhases * ((width + kCopySlice - 1) / kCopySlice), n = (units + waves - 1) / waves;
     return n < 1024 ? n : 1024;
 }
 template <class S> __device__ __forceinline__ void copy_empties(const int64_t *rowptr, int64_t seqs, int64_t tokens, int64_t width, const S *in, S *out,
                                                                 int64_t wave, int64_t waves)
 {
-    const int64_t slices = (width + kCopySlice - 1) / kCopySlice, units = (seqs + kWave - 1) / kWave * slices;
+    constexpr int kEach = kCopySlice / kWave;
+    const int64_t slices = (width + kCopySlice - 1) / kCopySlice, units = (seqs + kWave - 1) / kWave * kCopyPhases * slices;
     for (int64_t unit = wave; unit < units; unit += waves) {
-        const int64_t block = divide(unit, slices), from = (unit - block * slices) * kCopySlice, q = block * kWave + lane_id();
+        const int64_t some_of = divide(unit, slices), block = some_of / kCopyPhases, from = (unit - some_of * slices) * kCopySlice, q = block * kWave + lane_id();
+        const int phase = (int)(some_of % kCopyPhases);
         const bool empty = q < seqs && row_bound(rowptr[q], tokens) >= row_bound(rowptr[q + 1], tokens);
-        for (u64 some = __ballot(empty); some; some &= some - 1) {
-            const int64_t at = (block * kWave + __builtin_ctzll(some)) * width + from + lane_id();
-            const int64_t left = width - from - lane_id();
+        int number = 0;
+        for (u64 some = __ballot(empty); some; some &= some - 1, number++) {
+            if (number % kCopyPhases != phase) continue;
+            const int64_t at = (block * kWave + __builtin_ctzll(some)) * width + from + lane_id(), left = width - from - lane_id();
+            S v[kEach];
 #pragma unroll
-            for (int k = 0; k < kCopySlice / kWave; k++)
-                if (k * kWave < left) out[at + k * kWave] = in ? in[at + k * kWave] : (S)0.0f;
+            for (int k = 0; k < kEach; k++) v[k] = in && k * kWave < left ? in[at + k * kWave] : (S)0.0f;
+#pragma unroll
+            for (int k = 0; k < kEach; k++) if (k * kWave < left) out[at + k * kWave] = v[k];
         }
     }
 }

@@ -116,12 +116,32 @@ template <int S, int L> struct Lane {
     __device__ __forceinline__ void load(const SelectArgs &a, const float *p, int64_t row, float (&h)[S]) const
     {
         const float *at = p + (row * a.channels + c) * a.states + n0;
+        if (p && a.states % 4 == 0) {
+#pragma unroll
+            for (int i = 0; i < S; i += 4) {
+                Pack<F32, 4> v = {};
+                if (i < count) v.load(at + i);
+#pragma unroll
+                for (int k = 0; k < 4; k++) h[i + k] = v.get(k);
+            }
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < S; i++) h[i] = p && i < count ? at[i] : 0.0f;
     }
     __device__ __forceinline__ void store(const SelectArgs &a, float *p, int64_t row, const float (&h)[S]) const
     {
         float *at = p + (row * a.channels + c) * a.states + n0;
+        if (a.states % 4 == 0) {
+#pragma unroll
+            for (int i = 0; i < S; i += 4) {
+                const float some[4] = {h[i], h[i + 1], h[i + 2], h[i + 3]};
+                Pack<F32, 4> v;
+                v.set(some);
+                if (active && i < count) v.store(at + i);
+            }
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < S; i++) if (active && i < count) at[i] = h[i];
     }

@@ -199,8 +199,9 @@ void select_forward(int dtype, const SelectArgs &a, const SelectLayout &l, hipSt
 #undef DGN_CALL
 }
 
-// One token for each row: lanes as above, of a row's channel block.
-template <class T, int L>
+// One token for each row: four states a lane, of a row's channel block.  Bound by memory; what it reads is asked for before anything is
+// made of it.  kFours: a multiple of four states.
+template <class T, int L, bool kFours>
 __global__ __launch_bounds__(256) void k_select_step(SelectStepArgs s)
 {
     constexpr int S = 4;
@@ -212,26 +213,36 @@ __global__ __launch_bounds__(256) void k_select_step(SelectStepArgs s)
         ln.place(a, number - row * a.blocks);
         float y = 0.0f;
         if (slot >= 0 && slot < s.slots) {
-            float A2[S], h[S];
+            float A2[S], h[S], b[S], c[S];
             ln.load(a, s.state_in, slot, h);
+            const E delta = static_cast<const E *>(a.delta)[row * a.delta_stride + ln.c], xe = static_cast<const E *>(a.x)[row * a.x_stride + ln.c],
+                    ze = a.z ? static_cast<const E *>(a.z)[row * a.z_stride + ln.c] : (E)0.0f;
+            const E *be = static_cast<const E *>(a.B) + row * a.b_stride + ln.group * a.states + ln.n0,
+                    *ce = static_cast<const E *>(a.C) + row * a.c_stride + ln.group * a.states + ln.n0;
+            if (kFours) {
+                Pack<T, S> bs = {}, cs = {};
+                if (ln.count) {
+                    bs.load(be);
+                    cs.load(ce);
+                }
+#pragma unroll
+                for (int i = 0; i < S; i++) b[i] = bs.get(i), c[i] = cs.get(i);
+            } else {
+#pragma unroll
+                for (int i = 0; i < S; i++) b[i] = i < ln.count ? (float)be[i] : 0.0f, c[i] = i < ln.count ? (float)ce[i] : 0.0f;
+            }
             ln.decays(a, A2);
-            const float d = step_of((float)static_cast<const E *>(a.delta)[row * a.delta_stride + ln.c] + (a.delta_bias ? a.delta_bias[ln.c] : 0.0f));
-            const float x = (float)static_cast<const E *>(a.x)[row * a.x_stride + ln.c], u = d * x;
-            const E *b = static_cast<const E *>(a.B) + row * a.b_stride + ln.group * a.states + ln.n0,
-                    *c = static_cast<const E *>(a.C) + row * a.c_stride + ln.group * a.states + ln.n0;
+            const float bias = a.delta_bias ? a.delta_bias[ln.c] : 0.0f, D = a.D ? a.D[ln.c] : 0.0f;
+            const float d = step_of((float)delta + bias), x = (float)xe, u = d * x, z = (float)ze;
 #pragma unroll
             for (int i = 0; i < S; i++) {
-                const float bi = i < ln.count ? (float)b[i] : 0.0f, ci = i < ln.count ? (float)c[i] : 0.0f;
-                h[i] = fmaf(exp2_of(d * A2[i]), h[i], u * bi);
-                y = fmaf(ci, h[i], y);
+                h[i] = fmaf(exp2_of(d * A2[i]), h[i], u * b[i]);
+                y = fmaf(c[i], h[i], y);
             }
             ln.store(a, s.state_out, slot, h);
             y = sum_channel<L>(y);
-            if (a.D) y = fmaf(a.D[ln.c], x, y);
-            if (a.z) {
-                const float z = (float)static_cast<const E *>(a.z)[row * a.z_stride + ln.c];
-                y *= z * gate_of<T>(z);
-            }
+            if (a.D) y = fmaf(D, x, y);
+            if (a.z) y *= z * gate_of<T>(z);
         }
         if (ln.active && ln.part == 0) static_cast<E *>(a.y)[row * a.y_stride + ln.c] = (E)y;
     }
@@ -326,7 +337,11 @@ hipError_t launch_select_step(int dtype, const SelectStepArgs &args, hipStream_t
     a.in.blocks = a.in.group_blocks * a.in.groups;
     const int64_t n = (a.in.tokens * a.in.blocks + 3) / 4;
     const dim3 grid((unsigned)(n < (1 << 22) ? n : 1 << 22)), threads(256);
-#define DGN_CALL(S, L) hipLaunchKernelGGL((k_select_step<Type, L>), grid, threads, 0, s, a)
+#define DGN_CALL(S, L)                                                                                          \
+    do {                                                                                                        \
+        if (a.in.states % 4 == 0) hipLaunchKernelGGL((k_select_step<Type, L, true>), grid, threads, 0, s, a);   \
+        else hipLaunchKernelGGL((k_select_step<Type, L, false>), grid, threads, 0, s, a);                       \
+    } while (0)
 #define DGN_GO(T)                                   \
     do {                                            \
         typedef T Type;                             \
