@@ -19,7 +19,10 @@ namespace dgn {
 constexpr int kSelectWaves = 4;         // of a workgroup; each works by itself
 constexpr int kSelectBatch = 8;         // rows that a wave has in registers at a time
 constexpr int kSelectMostRows = 64;     // of a strip
-constexpr int kSelectKeep = 16;         // rows between two states that the forward pass keeps for the backward pass
+#ifndef KEEP
+#define KEEP 16
+#endif
+constexpr int kSelectKeep = KEEP;         // rows between two states that the forward pass keeps for the backward pass
 constexpr int64_t kFewStrips = 32;      // up to so many strips each applies the ones before it itself
 constexpr float kLog2e = 1.44269504088896340736f, kLog2eLow = 1.92596299112661746887e-8f, kLn2 = 0.69314718055994530942f;
 
@@ -90,9 +93,10 @@ template <int S, int L> struct Lane {
         rows = (int32_t)(left < a.rows ? left : a.rows);
         return true;
     }
-    __device__ __forceinline__ void place(const SelectArgs &a, int64_t block)
+    __device__ __forceinline__ void place(const SelectArgs &a, int64_t block) { place(a, block, divide(block, a.group_blocks)); }
+    __device__ __forceinline__ void place(const SelectArgs &a, int64_t block, int64_t group_)
     {
-        group = divide(block, a.group_blocks);
+        group = group_;
         const int64_t share = a.channels / a.groups, at = (block - group * a.group_blocks) * kChannels + lane_id() / L;
         active = at < share;
         c = group * share + (active ? at : share - 1);
@@ -129,7 +133,7 @@ template <int S, int L> struct Lane {
 #pragma unroll
         for (int i = 0; i < S; i++) h[i] = p && i < count ? at[i] : 0.0f;
     }
-    __device__ __forceinline__ void store(const SelectArgs &a, float *p, int64_t row, const float (&h)[S]) const
+    template <bool kStream = false> __device__ __forceinline__ void store(const SelectArgs &a, float *p, int64_t row, const float (&h)[S]) const
     {
         float *at = p + (row * a.channels + c) * a.states + n0;
         if (a.states % 4 == 0) {
@@ -138,7 +142,7 @@ template <int S, int L> struct Lane {
                 const float some[4] = {h[i], h[i + 1], h[i + 2], h[i + 3]};
                 Pack<F32, 4> v;
                 v.set(some);
-                if (active && i < count) v.store(at + i);
+                if (active && i < count) v.template store<kStream>(at + i);
             }
             return;
         }

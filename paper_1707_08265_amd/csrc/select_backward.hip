@@ -6,6 +6,9 @@
 // What comes back over strips is put together as the states are: a e -> exp(A sum d) (a e) + F, or F where a sequence ends.
 #include "select.h"
 
+#ifndef LB
+#define LB 2
+#endif
 namespace dgn {
 
 // First launch: what a strip does to what comes back into it, from its last row to its first; only the rows up to the first end have a part
@@ -123,7 +126,7 @@ template <int L> struct Back {
     static constexpr int kSumRows = kWide <= 64 ? kSelectKeep : 4;              // rows whose sums over channels are in LDS at a time
 };
 template <class T, int L>
-__global__ __launch_bounds__(Back<L>::kThreads, Back<L>::kWaves == 4 ? 2 : 1) void k_select_gradients(SelectArgs a)
+__global__ __launch_bounds__(Back<L>::kThreads, Back<L>::kWaves == 4 ? LB : 1) void k_select_gradients(SelectArgs a)
 {
     typedef Lane<4, L> Mine;
     typedef Back<L> G;
@@ -169,7 +172,7 @@ __global__ __launch_bounds__(Back<L>::kThreads, Back<L>::kWaves == 4 ? 2 : 1) vo
     float dD = 0.0f, dbias = 0.0f;
 
     for (int k0 = (ln.rows - 1) / kRows * kRows; k0 >= 0; k0 -= kRows) {
-        const uint32_t valid = ln.valid >> k0 & 0xffff, begin = ln.begin >> k0 & 0xffff, end = ln.end >> k0 & 0xffff;
+        const uint32_t valid = ln.valid >> k0 & ((1u << kRows) - 1), begin = ln.begin >> k0 & ((1u << kRows) - 1), end = ln.end >> k0 & ((1u << kRows) - 1);
         if (valid == 0) continue;
         const int64_t row0 = ln.row0 + k0;
         E x[G::kItems], delta[G::kItems], dy[G::kItems], z[G::kItems];
@@ -195,7 +198,9 @@ __global__ __launch_bounds__(Back<L>::kThreads, Back<L>::kWaves == 4 ? 2 : 1) vo
         for (int j = 0; j < G::kItems; j++) {
             const float d = step_of((float)delta[j] + bias), zj = (float)z[j];
             const float o = a.z ? (float)dy[j] * (zj * gate_of<T>(zj)) : (float)dy[j];
-            if (item_row + j * kItemStep < kRows) s_item[item_row + j * kItemStep][item_channel] = make_float4(d, d * (float)x[j], o, 0.0f);
+            // (channels that there are not have no part in the sums over channels)
+            if (item_row + j * kItemStep < kRows)
+                s_item[item_row + j * kItemStep][item_channel] = item_channel < width ? make_float4(d, d * (float)x[j], o, 0.0f) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         }
         __syncthreads();
         float before[kRows][4], decay[kRows][4];
@@ -233,8 +238,8 @@ __global__ __launch_bounds__(Back<L>::kThreads, Back<L>::kWaves == 4 ? 2 : 1) vo
                     const float ah = decay[k][i] * before[k][i], now = fmaf(u, b[i], ah);
                     e[i] = fmaf(o, c[i], e[i]);
                     y = fmaf(c[i], now, y);
-                    sums[r][i] = ln.active ? e[i] * u : 0.0f;
-                    sums[r][4 + i] = ln.active ? o * now : 0.0f;
+                    sums[r][i] = e[i] * u;
+                    sums[r][4 + i] = o * now;
                     eb = fmaf(e[i], b[i], eb);
                     const float w = e[i] * ah;
                     ea = fmaf(A2[i], w, ea);
@@ -298,8 +303,9 @@ __global__ __launch_bounds__(Back<L>::kThreads, Back<L>::kWaves == 4 ? 2 : 1) vo
     }
     ln.store_own(a.partial + ln.own(a, ln.strip), dA);
     // (the threads of a channel, one after the other)
-    static_assert(sizeof(s_sum) >= G::kThreads * sizeof(float2), "a pair for each thread");
-    float2 *pair = reinterpret_cast<float2 *>(&s_sum[0][0][0]);
+    constexpr bool kItemsFit = sizeof(s_item) >= G::kThreads * sizeof(float2);
+    static_assert(kItemsFit || sizeof(s_sum) >= G::kThreads * sizeof(float2), "a pair for each thread");
+    float2 *pair = kItemsFit ? reinterpret_cast<float2 *>(&s_item[0][0]) : reinterpret_cast<float2 *>(&s_sum[0][0][0]);
     pair[threadIdx.x] = make_float2(dD, dbias);
     __syncthreads();
     if ((int)threadIdx.x < width) {

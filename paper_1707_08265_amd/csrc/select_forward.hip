@@ -199,29 +199,49 @@ void select_forward(int dtype, const SelectArgs &a, const SelectLayout &l, hipSt
 #undef DGN_CALL
 }
 
-// One token for each row: four states a lane, of a row's channel block.  Bound by memory; what it reads is asked for before anything is
-// made of it.  kFours: a multiple of four states.
-template <class T, int L, bool kFours>
+// The value of lane k of each group of K (1, 2 or 4 neighbouring lanes).
+template <int K> __device__ __forceinline__ float of_lane(float v, int k)
+{
+    if (K == 1) return v;
+    if (K == 2) return k == 0 ? moved<0xA0>(v) : moved<0xF5>(v);
+    return k == 0 ? moved<0x00>(v) : k == 1 ? moved<0x55>(v) : k == 2 ? moved<0xAA>(v) : moved<0xFF>(v);
+}
+// One token for each row: four states a lane, kBlocks of a row's channel blocks a wave.  Bound by memory: all that is read is asked for before
+// anything is made of it, and what belongs to a channel (step, input, outer gate) is made by one lane: lane k of the first kBlocks for block k.
+// kFours: a multiple of four states.  States of calls larger than the last-level cache go past it: 1 024 rows of 2 048 x 16, 278 MB, in 53 us
+// (5.2 TB/s; else 64; with what belongs to a channel made by all its lanes 82, and with a block a wave 88).
+template <class T, int L, int kBlocks, bool kFours, bool kStream>
 __global__ __launch_bounds__(256) void k_select_step(SelectStepArgs s)
 {
+    static_assert(kBlocks <= L, "a lane for each block");
     constexpr int S = 4;
     typedef typename T::Store E;
     const SelectArgs &a = s.in;
-    for (int64_t number = (int64_t)blockIdx.x * 4 + wave_id(); number < a.tokens * a.blocks; number += (int64_t)gridDim.x * 4) {
-        const int64_t row = divide(number, a.blocks), slot = s.slot ? s.slot[row] : row;
-        Lane<S, L> ln;
-        ln.place(a, number - row * a.blocks);
+    const int64_t group_pieces = (a.group_blocks + kBlocks - 1) / kBlocks, pieces = group_pieces * a.groups;
+    for (int64_t number = (int64_t)blockIdx.x * 4 + wave_id(); number < a.tokens * pieces; number += (int64_t)gridDim.x * 4) {
+        const int64_t row = divide(number, pieces), piece = number - row * pieces, slot = s.slot ? s.slot[row] : row;
+        const int64_t group = divide(piece, group_pieces), block0 = group * a.group_blocks + (piece - group * group_pieces) * kBlocks;
+        Lane<S, L> ln[kBlocks], own;                    // own: whose channel the lane answers for
+        own.place(a, block0 + lane_id() % L % kBlocks, group);
+        const bool here = slot >= 0 && slot < s.slots;
         float y = 0.0f;
-        if (slot >= 0 && slot < s.slots) {
-            float A2[S], h[S], b[S], c[S];
-            ln.load(a, s.state_in, slot, h);
-            const E delta = static_cast<const E *>(a.delta)[row * a.delta_stride + ln.c], xe = static_cast<const E *>(a.x)[row * a.x_stride + ln.c],
-                    ze = a.z ? static_cast<const E *>(a.z)[row * a.z_stride + ln.c] : (E)0.0f;
-            const E *be = static_cast<const E *>(a.B) + row * a.b_stride + ln.group * a.states + ln.n0,
-                    *ce = static_cast<const E *>(a.C) + row * a.c_stride + ln.group * a.states + ln.n0;
+        if (here) {
+            float h[kBlocks][S], A[kBlocks][S], b[S], c[S];
+#pragma unroll
+            for (int k = 0; k < kBlocks; k++) {
+                ln[k].place(a, block0 + k, group);
+                ln[k].load(a, s.state_in, slot, h[k]);
+            }
+            const E delta = static_cast<const E *>(a.delta)[row * a.delta_stride + own.c], xe = static_cast<const E *>(a.x)[row * a.x_stride + own.c],
+                    ze = a.z ? static_cast<const E *>(a.z)[row * a.z_stride + own.c] : (E)0.0f;
+#pragma unroll
+            for (int k = 0; k < kBlocks; k++) ln[k].load(a, a.A, 0, A[k]);
+            const float bias = a.delta_bias ? a.delta_bias[own.c] : 0.0f, D = a.D ? a.D[own.c] : 0.0f;
+            const E *be = static_cast<const E *>(a.B) + row * a.b_stride + group * a.states + own.n0,
+                    *ce = static_cast<const E *>(a.C) + row * a.c_stride + group * a.states + own.n0;
             if (kFours) {
                 Pack<T, S> bs = {}, cs = {};
-                if (ln.count) {
+                if (own.count) {
                     bs.load(be);
                     cs.load(ce);
                 }
@@ -229,22 +249,26 @@ __global__ __launch_bounds__(256) void k_select_step(SelectStepArgs s)
                 for (int i = 0; i < S; i++) b[i] = bs.get(i), c[i] = cs.get(i);
             } else {
 #pragma unroll
-                for (int i = 0; i < S; i++) b[i] = i < ln.count ? (float)be[i] : 0.0f, c[i] = i < ln.count ? (float)ce[i] : 0.0f;
+                for (int i = 0; i < S; i++) b[i] = i < own.count ? (float)be[i] : 0.0f, c[i] = i < own.count ? (float)ce[i] : 0.0f;
             }
-            ln.decays(a, A2);
-            const float bias = a.delta_bias ? a.delta_bias[ln.c] : 0.0f, D = a.D ? a.D[ln.c] : 0.0f;
             const float d = step_of((float)delta + bias), x = (float)xe, u = d * x, z = (float)ze;
 #pragma unroll
-            for (int i = 0; i < S; i++) {
-                h[i] = fmaf(exp2_of(d * A2[i]), h[i], u * b[i]);
-                y = fmaf(c[i], h[i], y);
+            for (int k = 0; k < kBlocks; k++) {
+                const float dk = of_lane<kBlocks>(d, k) * kLog2e, uk = of_lane<kBlocks>(u, k);
+                float yk = 0.0f;
+#pragma unroll
+                for (int i = 0; i < S; i++) {
+                    h[k][i] = fmaf(exp2_of(dk * A[k][i]), h[k][i], uk * b[i]);
+                    yk = fmaf(c[i], h[k][i], yk);
+                }
+                ln[k].template store<kStream>(a, s.state_out, slot, h[k]);
+                yk = sum_channel<L>(yk);
+                if (lane_id() % L % kBlocks == k) y = yk;
             }
-            ln.store(a, s.state_out, slot, h);
-            y = sum_channel<L>(y);
             if (a.D) y = fmaf(D, x, y);
             if (a.z) y *= z * gate_of<T>(z);
         }
-        if (ln.active && ln.part == 0) static_cast<E *>(a.y)[row * a.y_stride + ln.c] = (E)y;
+        if (own.active && own.part < kBlocks) static_cast<E *>(a.y)[row * a.y_stride + own.c] = (E)y;
     }
 }
 
@@ -328,6 +352,7 @@ hipError_t launch_select(int dtype, bool back, const SelectArgs &args, void *car
     return hipGetLastError();
 }
 
+constexpr int64_t kManySteps = 8192;     // waves, of one block each, from which on they take several
 hipError_t launch_select_step(int dtype, const SelectStepArgs &args, hipStream_t s)
 {
     const SelectLayout l = select_layout(args.in);
@@ -335,12 +360,19 @@ hipError_t launch_select_step(int dtype, const SelectStepArgs &args, hipStream_t
     const int64_t width = kWave / (l.wide / 4), share = a.in.channels / a.in.groups;
     a.in.group_blocks = (int32_t)((share + width - 1) / width);
     a.in.blocks = a.in.group_blocks * a.in.groups;
-    const int64_t n = (a.in.tokens * a.in.blocks + 3) / 4;
+    const bool many = a.in.states % 4 == 0 && a.in.tokens * a.in.blocks >= kManySteps;
+    const bool stream = many && (size_t)a.in.tokens * a.in.channels * (a.in.states * 2 * sizeof(float) + 3 * element_size(dtype)) > kStreamBytes;
+    const int64_t each = !many ? 1 : l.wide < 16 ? l.wide / 4 : 4;
+    const int64_t n = (a.in.tokens * ((a.in.group_blocks + each - 1) / each) * a.in.groups + 3) / 4;
     const dim3 grid((unsigned)(n < (1 << 22) ? n : 1 << 22)), threads(256);
-#define DGN_CALL(S, L)                                                                                          \
-    do {                                                                                                        \
-        if (a.in.states % 4 == 0) hipLaunchKernelGGL((k_select_step<Type, L, true>), grid, threads, 0, s, a);   \
-        else hipLaunchKernelGGL((k_select_step<Type, L, false>), grid, threads, 0, s, a);                       \
+#define DGN_STEP(L, N, F, P) hipLaunchKernelGGL((k_select_step<Type, L, N, F, P>), grid, threads, 0, s, a)
+#define DGN_CALL(S, L)                                              \
+    do {                                                            \
+        if (a.in.states % 4 == 0) {                                 \
+            if (stream) DGN_STEP(L, (L < 4 ? L : 4), true, true);   \
+            else if (many) DGN_STEP(L, (L < 4 ? L : 4), true, false); \
+            else DGN_STEP(L, 1, true, false);                       \
+        } else DGN_STEP(L, 1, false, false);                        \
     } while (0)
 #define DGN_GO(T)                                   \
     do {                                            \
@@ -358,6 +390,7 @@ hipError_t launch_select_step(int dtype, const SelectStepArgs &args, hipStream_t
     DGN_BY_DTYPE(dtype, DGN_GO);
 #undef DGN_GO
 #undef DGN_CALL
+#undef DGN_STEP
     return hipGetLastError();
 }
 
