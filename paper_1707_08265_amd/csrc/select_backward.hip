@@ -203,81 +203,88 @@ __global__ __launch_bounds__(Back<L>::kThreads, Back<L>::kWaves == 4 ? LB : 1) v
                 s_item[item_row + j * kItemStep][item_channel] = item_channel < width ? make_float4(d, d * (float)x[j], o, 0.0f) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         }
         __syncthreads();
-        float before[kRows][4], decay[kRows][4];
+        const auto rows = [&](auto inside) {
+            float before[kRows][4], decay[kRows][4];
 #pragma unroll
-        for (int k = 0; k < kRows; k++) {
-            if (!(valid >> k & 1)) continue;
-            const float2 du = *reinterpret_cast<const float2 *>(&s_item[k][lane_channel]);
-            float b[4];
-            take_states(s_bc[0] + k * kWide + ln.n0, b);
-            if (begin >> k & 1) ln.load(a, a.h0, ln.q(k0 + k), h);
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                before[k][i] = h[i];
-                decay[k][i] = exp2_of(du.x * A2[i]);
-                h[i] = fmaf(decay[k][i], h[i], du.y * b[i]);
-            }
-        }
-#pragma unroll
-        for (int k4 = kRows - 4; k4 >= 0; k4 -= 4) {
-            float sums[4][8];
-#pragma unroll
-            for (int r = 3; r >= 0; r--) {
-                const int k = k4 + r;
-#pragma unroll
-                for (int i = 0; i < 8; i++) sums[r][i] = 0.0f;
-                if (!(valid >> k & 1)) continue;
-                const float4 it = s_item[k][lane_channel];
-                const float d = it.x, u = it.y, o = it.z;
-                float b[4], c[4], y = 0.0f, eb = 0.0f, ea = 0.0f;
+            for (int k = 0; k < kRows; k++) {
+                if (!inside.value && !(valid >> k & 1)) continue;
+                const float2 du = *reinterpret_cast<const float2 *>(&s_item[k][lane_channel]);
+                float b[4];
                 take_states(s_bc[0] + k * kWide + ln.n0, b);
-                take_states(s_bc[1] + k * kWide + ln.n0, c);
-                if (end >> k & 1) ln.load(a, a.dfinal, ln.q(k0 + k), e);
+                if (!inside.value && (begin >> k & 1)) ln.load(a, a.h0, ln.q(k0 + k), h);
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
-                    const float ah = decay[k][i] * before[k][i], now = fmaf(u, b[i], ah);
-                    e[i] = fmaf(o, c[i], e[i]);
-                    y = fmaf(c[i], now, y);
-                    sums[r][i] = e[i] * u;
-                    sums[r][4 + i] = o * now;
-                    eb = fmaf(e[i], b[i], eb);
-                    const float w = e[i] * ah;
-                    ea = fmaf(A2[i], w, ea);
-                    dA[i] = fmaf(d, w, dA[i]);
-                    e[i] *= decay[k][i];
+                    before[k][i] = h[i];
+                    decay[k][i] = exp2_of(du.x * A2[i]);
+                    h[i] = fmaf(decay[k][i], h[i], du.y * b[i]);
                 }
-                y = sum_channel<L>(y);
-                eb = sum_channel<L>(eb);
-                ea = sum_channel<L>(ea);
-                wave_fence();
-                if (ln.part == 0) *reinterpret_cast<float4 *>(&s_item[k][lane_channel]) = make_float4(eb, ea * kLn2, y, d);
-                if ((begin >> k & 1) && a.dh0) ln.store(a, a.dh0, ln.q(k0 + k), e);
             }
-            sum_rows<L>(sums);
-            // (lanes of the same states hold the same sums: those of the first channel of their part of the wave write)
-            constexpr int kLeft = L <= 16 ? 1 : L <= 32 ? 2 : 4, kPart = L <= 16 ? 16 : L <= 32 ? 32 : 64;
-            const int first = k4 % G::kSumRows + (L <= 32 ? lane_id() / 32 * 2 : 0) + (L <= 16 ? lane_id() / 16 % 2 : 0);
-            if (lane_id() % kPart < L) {
 #pragma unroll
-                for (int r = 0; r < kLeft; r++) {
-                    float *to = s_sum[wave_id()][first + r];
-                    *reinterpret_cast<float4 *>(to + ln.n0) = make_float4(sums[r][0], sums[r][1], sums[r][2], sums[r][3]);
-                    *reinterpret_cast<float4 *>(to + kWide + ln.n0) = make_float4(sums[r][4], sums[r][5], sums[r][6], sums[r][7]);
-                }
-            }
-            if (k4 % G::kSumRows == 0) {
-                __syncthreads();
-                float *to = a.shared + part * a.tokens * a.groups * (2 * kWide) + ln.group * (2 * kWide);
-                for (int at = threadIdx.x; at < G::kSumRows * 2 * kWide; at += G::kThreads) {
-                    const int r = at / (2 * kWide), n = at % (2 * kWide);
-                    float sum = 0.0f;
+            for (int k4 = kRows - 4; k4 >= 0; k4 -= 4) {
+                float sums[4][8];
 #pragma unroll
-                    for (int w = 0; w < G::kWaves; w++) sum += s_sum[w][r][n];
-                    if (k0 + k4 + r < ln.rows) to[(row0 + k4 + r) * a.groups * (2 * kWide) + n] = sum;
+                for (int r = 3; r >= 0; r--) {
+                    const int k = k4 + r;
+                    if (!inside.value && !(valid >> k & 1)) {
+#pragma unroll
+                        for (int i = 0; i < 8; i++) sums[r][i] = 0.0f;
+                        continue;
+                    }
+                    const float4 it = s_item[k][lane_channel];
+                    const float d = it.x, u = it.y, o = it.z;
+                    float b[4], c[4], y = 0.0f, eb = 0.0f, ea = 0.0f;
+                    take_states(s_bc[0] + k * kWide + ln.n0, b);
+                    take_states(s_bc[1] + k * kWide + ln.n0, c);
+                    if (!inside.value && (end >> k & 1)) ln.load(a, a.dfinal, ln.q(k0 + k), e);
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const float ah = decay[k][i] * before[k][i], now = fmaf(u, b[i], ah);
+                        e[i] = fmaf(o, c[i], e[i]);
+                        y = fmaf(c[i], now, y);
+                        sums[r][i] = e[i] * u;
+                        sums[r][4 + i] = o * now;
+                        eb = fmaf(e[i], b[i], eb);
+                        const float w = e[i] * ah;
+                        ea = fmaf(A2[i], w, ea);
+                        dA[i] = fmaf(d, w, dA[i]);
+                        e[i] *= decay[k][i];
+                    }
+                    y = sum_channel<L>(y);
+                    eb = sum_channel<L>(eb);
+                    ea = sum_channel<L>(ea);
+                    wave_fence();
+                    if (ln.part == 0) *reinterpret_cast<float4 *>(&s_item[k][lane_channel]) = make_float4(eb, ea * kLn2, y, d);
+                    if (!inside.value && (begin >> k & 1) && a.dh0) ln.store(a, a.dh0, ln.q(k0 + k), e);
                 }
-                if (G::kSumRows < kRows) __syncthreads();
+                sum_rows<L>(sums);
+                // (lanes of the same states hold the same sums: those of the first channel of their part of the wave write)
+                constexpr int kLeft = L <= 16 ? 1 : L <= 32 ? 2 : 4, kPart = L <= 16 ? 16 : L <= 32 ? 32 : 64;
+                const int first = k4 % G::kSumRows + (L <= 32 ? lane_id() / 32 * 2 : 0) + (L <= 16 ? lane_id() / 16 % 2 : 0);
+                if (lane_id() % kPart < L) {
+#pragma unroll
+                    for (int r = 0; r < kLeft; r++) {
+                        float *to = s_sum[wave_id()][first + r];
+                        *reinterpret_cast<float4 *>(to + ln.n0) = make_float4(sums[r][0], sums[r][1], sums[r][2], sums[r][3]);
+                        *reinterpret_cast<float4 *>(to + kWide + ln.n0) = make_float4(sums[r][4], sums[r][5], sums[r][6], sums[r][7]);
+                    }
+                }
+                if (k4 % G::kSumRows == 0) {
+                    __syncthreads();
+                    float *to = a.shared + part * a.tokens * a.groups * (2 * kWide) + ln.group * (2 * kWide);
+                    for (int at = threadIdx.x; at < G::kSumRows * 2 * kWide; at += G::kThreads) {
+                        const int r = at / (2 * kWide), n = at % (2 * kWide);
+                        float sum = 0.0f;
+#pragma unroll
+                        for (int w = 0; w < G::kWaves; w++) sum += s_sum[w][r][n];
+                        if (inside.value || k0 + k4 + r < ln.rows) to[(row0 + k4 + r) * a.groups * (2 * kWide) + n] = sum;
+                    }
+                    if (G::kSumRows < kRows) __syncthreads();
+                }
             }
-        }
+        };
+        // (most rows are in the middle of a sequence: those ask for nothing, so that the next ones can be under way)
+        if (valid == (1u << kRows) - 1 && (begin | end) == 0) rows(std::true_type());
+        else rows(std::false_type());
         if (G::kSumRows < kRows) __syncthreads();
 #pragma unroll
         for (int j = 0; j < G::kItems; j++) {
