@@ -19,10 +19,7 @@ namespace dgn {
 constexpr int kSelectWaves = 4;         // of a workgroup; each works by itself
 constexpr int kSelectBatch = 8;         // rows that a wave has in registers at a time
 constexpr int kSelectMostRows = 64;     // of a strip
-#ifndef KEEP
-#define KEEP 16
-#endif
-constexpr int kSelectKeep = KEEP;         // rows between two states that the forward pass keeps for the backward pass
+constexpr int kSelectKeep = 16;         // rows between two states that the forward pass keeps for the backward pass
 constexpr int64_t kFewStrips = 32;      // up to so many strips each applies the ones before it itself
 constexpr float kLog2e = 1.44269504088896340736f, kLog2eLow = 1.92596299112661746887e-8f, kLn2 = 0.69314718055994530942f;
 
@@ -36,20 +33,17 @@ __device__ __forceinline__ float small_exp(float v)     // exp(-|v|)
     const float w = -fabsf(v), t = w * kLog2e, e = fmaf(w, kLog2eLow, fmaf(w, kLog2e, -t)), q = exp2_of(t);
     return t < -126.0f ? 0.0f : fmaf(q, e * kLn2, q);       // (w of -inf: e is NaN)
 }
-__device__ __forceinline__ float step_of(float v)
+struct Step { float d, slope; };
+__device__ __forceinline__ Step step_and_slope(float v)
 {
-    const float q = small_exp(v), s = q * inverse(2.0f + q), r = s * s;
+    const float q = small_exp(v), s = q * inverse(2.0f + q), r = s * s, k = inverse(1.0f + q);
     float p = fmaf(r, 0.13433805108070374f, 0.1411697268486023f);
     p = fmaf(r, p, 0.2000383585691452f);
     p = fmaf(r, p, 0.33333319425582886f);
     const float half = fmaf(s * r, p, s), positive = v > 0.0f ? v : 0.0f;
-    return fmaf(2.0f, half, positive);
+    return Step{fmaf(2.0f, half, positive), v > 0.0f ? k : q * k};
 }
-__device__ __forceinline__ float slope_of(float v)
-{
-    const float q = small_exp(v), k = inverse(1.0f + q);
-    return v > 0.0f ? k : q * k;
-}
+__device__ __forceinline__ float step_of(float v) { return step_and_slope(v).d; }
 // sigma(z): of 32 bits by a rounded exponential and quotient.
 template <class T> __device__ __forceinline__ float gate_of(float z)
 {
@@ -234,6 +228,16 @@ template <class T, int kRows> struct Column {
     }
     __device__ __forceinline__ float get(int k) const { return (float)v[k]; }
 };
+
+// The arguments of the kernel (its first parameter) from where the launch has put them.  They do not fit the scalar registers of a wave that
+// also has a loop's own values there; what a part of the loop needs of them it asks for anew, and the compiler does not keep it from part to part.
+__device__ __forceinline__ SelectArgs asked_again()
+{
+    typedef const __attribute__((address_space(4))) SelectArgs *At;
+    At p = (At)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const SelectArgs *)p;
+}
 
 // How lanes and strips are cut.
 struct SelectLayout {

@@ -6,9 +6,6 @@
 // What comes back over strips is put together as the states are: a e -> exp(A sum d) (a e) + F, or F where a sequence ends.
 #include "select.h"
 
-#ifndef LB
-#define LB 2
-#endif
 namespace dgn {
 
 // First launch: what a strip does to what comes back into it, from its last row to its first; only the rows up to the first end have a part
@@ -126,7 +123,7 @@ template <int L> struct Back {
     static constexpr int kSumRows = kWide <= 64 ? kSelectKeep : 4;              // rows whose sums over channels are in LDS at a time
 };
 template <class T, int L>
-__global__ __launch_bounds__(Back<L>::kThreads, Back<L>::kWaves == 4 ? LB : 1) void k_select_gradients(SelectArgs a)
+__global__ __launch_bounds__(Back<L>::kThreads, Back<L>::kWaves == 4 ? 2 : 1) void k_select_gradients(SelectArgs args)
 {
     typedef Lane<4, L> Mine;
     typedef Back<L> G;
@@ -136,6 +133,7 @@ __global__ __launch_bounds__(Back<L>::kThreads, Back<L>::kWaves == 4 ? LB : 1) v
     __shared__ float4 s_item[kRows][G::kChannels];                                // step, input, gradient; then sums of e B, A e a h, C h
     __shared__ __attribute__((aligned(16))) float s_bc[2][kRows * kWide];
     __shared__ __attribute__((aligned(16))) float s_sum[G::kWaves][G::kSumRows][2 * kWide];
+    const SelectArgs &a = args;
     const int64_t strips = a.strips * a.blocks;
     if (blockIdx.x >= strips) {
         if (a.dh0)
@@ -171,29 +169,53 @@ __global__ __launch_bounds__(Back<L>::kThreads, Back<L>::kWaves == 4 ? LB : 1) v
     const float bias = a.delta_bias ? a.delta_bias[ci] : 0.0f, D = a.D ? a.D[ci] : 0.0f;
     float dD = 0.0f, dbias = 0.0f;
 
-    for (int k0 = (ln.rows - 1) / kRows * kRows; k0 >= 0; k0 -= kRows) {
-        const uint32_t valid = ln.valid >> k0 & ((1u << kRows) - 1), begin = ln.begin >> k0 & ((1u << kRows) - 1), end = ln.end >> k0 & ((1u << kRows) - 1);
-        if (valid == 0) continue;
-        const int64_t row0 = ln.row0 + k0;
-        E x[G::kItems], delta[G::kItems], dy[G::kItems], z[G::kItems];
+    // what the next rows are made of: asked for while the ones after them are worked on
+    constexpr int kShared = (kRows * kWide + G::kThreads - 1) / G::kThreads;
+    E x1[G::kItems], delta1[G::kItems], dy1[G::kItems], z1[G::kItems], b1[kShared], c1[kShared];
+    float h1[4];
+    const auto fetch = [&](int64_t row0) {
+        const SelectArgs a = asked_again();
 #pragma unroll
         for (int j = 0; j < G::kItems; j++) {
             int64_t row = row0 + item_row + j * kItemStep;
             row = row < a.tokens ? row : a.tokens - 1;
-            x[j] = static_cast<const E *>(a.x)[row * a.x_stride + ci];
-            delta[j] = static_cast<const E *>(a.delta)[row * a.delta_stride + ci];
-            dy[j] = static_cast<const E *>(a.dy)[row * a.dy_stride + ci];
-            z[j] = a.z ? static_cast<const E *>(a.z)[row * a.z_stride + ci] : (E)0.0f;
+            x1[j] = static_cast<const E *>(a.x)[row * a.x_stride + ci];
+            delta1[j] = static_cast<const E *>(a.delta)[row * a.delta_stride + ci];
+            dy1[j] = static_cast<const E *>(a.dy)[row * a.dy_stride + ci];
+            z1[j] = a.z ? static_cast<const E *>(a.z)[row * a.z_stride + ci] : (E)0.0f;
         }
-        float h[4];
-        ln.load_own(a.kept + ln.own(a, row0 / kRows), h);
-        for (int at = threadIdx.x; at < kRows * kWide; at += G::kThreads) {
-            const int n = at % kWide;
+#pragma unroll
+        for (int j = 0; j < kShared; j++) {
+            const int at = j * G::kThreads + threadIdx.x, n = at % kWide;
             int64_t row = row0 + at / kWide;
             row = row < a.tokens ? row : a.tokens - 1;
-            s_bc[0][at] = n < a.states ? (float)static_cast<const E *>(a.B)[row * a.b_stride + ln.group * a.states + n] : 0.0f;
-            s_bc[1][at] = n < a.states ? (float)static_cast<const E *>(a.C)[row * a.c_stride + ln.group * a.states + n] : 0.0f;
+            b1[j] = n < a.states ? static_cast<const E *>(a.B)[row * a.b_stride + ln.group * a.states + n] : (E)0.0f;
+            c1[j] = n < a.states ? static_cast<const E *>(a.C)[row * a.c_stride + ln.group * a.states + n] : (E)0.0f;
         }
+        ln.load_own(a.kept + ln.own(a, row0 / kRows), h1);
+    };
+    const int top = (ln.rows - 1) / kRows * kRows;
+    fetch(ln.row0 + top);
+    for (int k0 = top; k0 >= 0; k0 -= kRows) {
+        const uint32_t valid = ln.valid >> k0 & ((1u << kRows) - 1), begin = ln.begin >> k0 & ((1u << kRows) - 1), end = ln.end >> k0 & ((1u << kRows) - 1);
+        const int64_t row0 = ln.row0 + k0;
+        E x[G::kItems], delta[G::kItems], dy[G::kItems], z[G::kItems];
+        float h[4];
+#pragma unroll
+        for (int j = 0; j < G::kItems; j++) x[j] = x1[j], delta[j] = delta1[j], dy[j] = dy1[j], z[j] = z1[j];
+#pragma unroll
+        for (int i = 0; i < 4; i++) h[i] = h1[i];
+#pragma unroll
+        for (int j = 0; j < kShared; j++) {
+            const int at = j * G::kThreads + threadIdx.x;
+            if (kShared * G::kThreads == kRows * kWide || at < kRows * kWide) {
+                s_bc[0][at] = (float)b1[j];
+                s_bc[1][at] = (float)c1[j];
+            }
+        }
+        if (k0 > 0) fetch(row0 - kRows);
+        if (valid == 0) { __syncthreads(); continue; }
+        const SelectArgs a = asked_again();
 #pragma unroll
         for (int j = 0; j < G::kItems; j++) {
             const float d = step_of((float)delta[j] + bias), zj = (float)z[j];
@@ -204,6 +226,7 @@ __global__ __launch_bounds__(Back<L>::kThreads, Back<L>::kWaves == 4 ? LB : 1) v
         }
         __syncthreads();
         const auto rows = [&](auto inside) {
+            const SelectArgs a = asked_again();
             float before[kRows][4], decay[kRows][4];
 #pragma unroll
             for (int k = 0; k < kRows; k++) {
@@ -286,6 +309,7 @@ __global__ __launch_bounds__(Back<L>::kThreads, Back<L>::kWaves == 4 ? LB : 1) v
         if (valid == (1u << kRows) - 1 && (begin | end) == 0) rows(std::true_type());
         else rows(std::false_type());
         if (G::kSumRows < kRows) __syncthreads();
+        const SelectArgs b = asked_again();
 #pragma unroll
         for (int j = 0; j < G::kItems; j++) {
             const int k = item_row + j * kItemStep;
@@ -294,15 +318,15 @@ __global__ __launch_bounds__(Back<L>::kThreads, Back<L>::kWaves == 4 ? LB : 1) v
             const float4 got = s_item[k][item_channel];
             const float xj = (float)x[j], dyj = (float)dy[j], zj = (float)z[j], eb = got.x, d = got.w;
             float o = dyj, y = got.z;
-            if (a.D) y = fmaf(D, xj, y);
-            if (a.z) {
+            if (b.D) y = fmaf(D, xj, y);
+            if (b.z) {
                 const float s = gate_of<T>(zj);
                 o = dyj * (zj * s);
-                static_cast<E *>(a.dz)[row * a.dz_stride + ci] = (E)(dyj * y * (s * fmaf(zj, 1.0f - s, 1.0f)));
+                static_cast<E *>(b.dz)[row * b.dz_stride + ci] = (E)(dyj * y * (s * fmaf(zj, 1.0f - s, 1.0f)));
             }
-            const float dx = a.D ? fmaf(D, o, d * eb) : d * eb, dd = fmaf(eb, xj, got.y) * slope_of((float)delta[j] + bias);
-            static_cast<E *>(a.dx)[row * a.dx_stride + ci] = (E)dx;
-            static_cast<E *>(a.ddelta)[row * a.ddelta_stride + ci] = (E)dd;
+            const float dx = b.D ? fmaf(D, o, d * eb) : d * eb, dd = fmaf(eb, xj, got.y) * step_and_slope((float)delta[j] + bias).slope;
+            static_cast<E *>(b.dx)[row * b.dx_stride + ci] = (E)dx;
+            static_cast<E *>(b.ddelta)[row * b.ddelta_stride + ci] = (E)dd;
             dD = fmaf(o, xj, dD);
             dbias += dd;
         }

@@ -61,49 +61,80 @@ __global__ __launch_bounds__(kSelectWaves *kWave) void k_select_ends(SelectArgs 
     if (ln.active && ln.part == 0) a.spans[ln.strip * a.channels + ln.c] = span;
 }
 
-// Second launch: the state that comes into each strip.  A workgroup has 64 states (a wave reads 64 neighbours of a strip) and kPieces pieces of
-// the strips: each is put together, the pieces before are applied one after the other, and each is gone through again.
-constexpr int kPieces = 16;
-__global__ __launch_bounds__(kPieces *kWave) void k_select_states(SelectArgs a, int wide, bool back)
+// Second launch: the state that comes into each strip.  A workgroup has kSlots neighbouring states and 1 024 / kSlots pieces of the strips: each
+// is put together, the pieces before are applied one after the other, and each is gone through again: up to kEach strips of a piece with what
+// they do in registers, so that it is asked for once and all at once (kEach 0: any number).  256 strips of 16 384 states: 29 us without.
+constexpr int kStateThreads = 1024;
+template <int kSlots, int kEach>
+__global__ __launch_bounds__(kStateThreads) void k_select_states(SelectArgs a, int wide, bool back)
 {
-    __shared__ float s_end[kPieces][kWave], s_span[kPieces][kWave];
+    constexpr int kPieces = kStateThreads / kSlots;
+    __shared__ float s_end[kPieces][kSlots], s_span[kPieces][kSlots];
     __shared__ bool s_cut[kPieces];
-    const int64_t slots = a.channels * wide, slot = (int64_t)blockIdx.x * kWave + lane_id(), at = slot < slots ? slot : slots - 1;
+    const int lane = threadIdx.x % kSlots, piece = threadIdx.x / kSlots;
+    const int64_t slots = a.channels * wide, slot = (int64_t)blockIdx.x * kSlots + lane, at = slot < slots ? slot : slots - 1;
     const int64_t c = divide(at, wide), n = at - c * wide;
     const float A2 = n < a.states ? a.A[c * a.states + n] * kLog2e : 0.0f;
-    const int piece = wave_id();
     const int64_t each = (a.strips + kPieces - 1) / kPieces, from = piece * each, to = from + each < a.strips ? from + each : a.strips;
-    float h = 0.0f, span = 0.0f;
-    bool cut = false;
     float *out = back ? a.back : a.before;
+    const auto strip_of = [&](int64_t k) { return back ? a.strips - 1 - k : k; };
+    float end[kEach ? kEach : 1], step[kEach ? kEach : 1];
+    uint32_t cuts = 0;
+    if (kEach) {
+        static_assert(kEach <= 16 && kEach <= kSlots, "a lane for each strip of a piece");
+#pragma unroll
+        for (int k = 0; k < kEach; k++) {
+            const int64_t strip = strip_of(from + k < to ? from + k : 0);
+            end[k] = a.ends[strip * slots + at];
+            step[k] = a.spans[strip * a.channels + c];
+        }
+        const bool cut = lane < kEach && from + lane < to && a.cuts[strip_of(from + lane < to ? from + lane : 0)];
+        cuts = (uint32_t)(__ballot(cut) >> (lane_id() & ~(kSlots < kWave ? kSlots - 1 : kWave - 1)));
+    }
+    float h = 0.0f, span = 0.0f;
+    bool any = cuts != 0;
     const auto every = [&](auto write) {
+        if (kEach) {
+#pragma unroll
+            for (int k = 0; k < kEach; k++) {
+                if (from + k >= to) break;
+                if (write.value) { if (slot < slots) out[strip_of(from + k) * slots + slot] = h; }
+                h = cuts >> k & 1 ? end[k] : fmaf(exp2_of(step[k] * A2), h, end[k]);
+                span += step[k];
+            }
+            return;
+        }
 #pragma unroll 4
         for (int64_t k = from; k < to; k++) {
-            const int64_t strip = back ? a.strips - 1 - k : k;
+            const int64_t strip = strip_of(k);
             const float e = a.ends[strip * slots + at], d = a.spans[strip * a.channels + c];
             const bool here = a.cuts[strip];
             if (write.value) { if (slot < slots) out[strip * slots + slot] = h; }
             h = here ? e : fmaf(exp2_of(d * A2), h, e);
             span += d;
-            cut = cut || here;
+            any = any || here;
         }
     };
     every(std::false_type());
-    s_end[piece][lane_id()] = h;
-    s_span[piece][lane_id()] = span;
-    if (lane_id() == 0) s_cut[piece] = cut;
+    s_end[piece][lane] = h;
+    s_span[piece][lane] = span;
+    if (lane == 0) s_cut[piece] = any;
     __syncthreads();
     h = 0.0f;
+#pragma unroll 4
     for (int p = 0; p < piece; p++) {
-        const float e = s_end[p][lane_id()];
-        h = s_cut[p] ? e : fmaf(exp2_of(s_span[p][lane_id()] * A2), h, e);
+        const float e = s_end[p][lane];
+        h = s_cut[p] ? e : fmaf(exp2_of(s_span[p][lane] * A2), h, e);
     }
     every(std::true_type());
 }
 void select_states(const SelectArgs &a, int wide, bool back, hipStream_t s)
 {
-    const int64_t groups = (a.channels * wide + kWave - 1) / kWave;
-    hipLaunchKernelGGL(k_select_states, dim3((unsigned)groups), dim3(kPieces * kWave), 0, s, a, wide, back);
+    const int64_t slots = a.channels * wide;
+    const dim3 threads(kStateThreads), few((unsigned)((slots + 63) / 64));
+    if (a.strips <= 64) hipLaunchKernelGGL((k_select_states<64, 4>), few, threads, 0, s, a, wide, back);
+    else if (a.strips <= 256) hipLaunchKernelGGL((k_select_states<64, 16>), few, threads, 0, s, a, wide, back);
+    else hipLaunchKernelGGL((k_select_states<64, 0>), few, threads, 0, s, a, wide, back);
 }
 
 // Third launch.
@@ -274,7 +305,7 @@ __global__ __launch_bounds__(256) void k_select_step(SelectStepArgs s)
 
 // Lanes: 16 states each where that gives enough waves, else four.  Rows of a strip: as few as give kSelectStrips waves, from kSelectKeep to
 // kSelectMostRows.
-constexpr int64_t kSelectStrips = 8192, kManyWaves = 2048;
+constexpr int64_t kSelectStrips = 4096, kManyWaves = 2048;
 SelectLayout select_layout(const SelectArgs &a)
 {
     SelectLayout l;
@@ -311,7 +342,7 @@ bool select_fits(int, const SelectArgs &a)          // launches of less than 2^3
 {
     const SelectLayout l = select_layout(a);
     const int64_t most = l.blocks > l.back_blocks ? l.blocks : l.back_blocks;
-    return l.strips * most < ((int64_t)1 << 25) && a.channels * l.wide < ((int64_t)1 << 27);
+    return l.strips * most < ((int64_t)1 << 24) && a.channels * l.wide < ((int64_t)1 << 25);
 }
 size_t select_scratch_bytes(int, const SelectArgs &a) { return select_layout(a).bytes; }
 size_t select_carry_bytes(int, const SelectArgs &a) { return select_layout(a).carry; }
