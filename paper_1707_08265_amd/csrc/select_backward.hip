@@ -162,10 +162,11 @@ __global__ __launch_bounds__(Back<L>::kThreads, Back<L>::kWaves == 4 ? 2 : 1) vo
     ln.mark(a, s_own[wave_id()]);
 
     // the thread's rows and channel where it makes what belongs to a row and channel
-    const int item_channel = threadIdx.x % G::kChannels, item_row = threadIdx.x / G::kChannels;
+    const int item_channel = threadIdx.x % G::kChannels, item_row = G::kChannels == kWave ? wave_id() : (int)threadIdx.x / G::kChannels;
     constexpr int kItemStep = G::kThreads / G::kChannels;
     const bool item = item_channel < width && item_row < kRows;
-    const int64_t ci = c0 + (item_channel < width ? item_channel : width - 1);
+    const uint32_t own = item_channel < width ? item_channel : width - 1;
+    const int64_t ci = c0 + own;
     const float bias = a.delta_bias ? a.delta_bias[ci] : 0.0f, D = a.D ? a.D[ci] : 0.0f;
     float dD = 0.0f, dbias = 0.0f;
 
@@ -179,10 +180,10 @@ __global__ __launch_bounds__(Back<L>::kThreads, Back<L>::kWaves == 4 ? 2 : 1) vo
         for (int j = 0; j < G::kItems; j++) {
             int64_t row = row0 + item_row + j * kItemStep;
             row = row < a.tokens ? row : a.tokens - 1;
-            x1[j] = static_cast<const E *>(a.x)[row * a.x_stride + ci];
-            delta1[j] = static_cast<const E *>(a.delta)[row * a.delta_stride + ci];
-            dy1[j] = static_cast<const E *>(a.dy)[row * a.dy_stride + ci];
-            z1[j] = a.z ? static_cast<const E *>(a.z)[row * a.z_stride + ci] : (E)0.0f;
+            x1[j] = (static_cast<const E *>(a.x) + row * a.x_stride + c0)[own];
+            delta1[j] = (static_cast<const E *>(a.delta) + row * a.delta_stride + c0)[own];
+            dy1[j] = (static_cast<const E *>(a.dy) + row * a.dy_stride + c0)[own];
+            z1[j] = a.z ? (static_cast<const E *>(a.z) + row * a.z_stride + c0)[own] : (E)0.0f;
         }
 #pragma unroll
         for (int j = 0; j < kShared; j++) {
@@ -200,7 +201,7 @@ __global__ __launch_bounds__(Back<L>::kThreads, Back<L>::kWaves == 4 ? 2 : 1) vo
         const uint32_t valid = ln.valid >> k0 & ((1u << kRows) - 1), begin = ln.begin >> k0 & ((1u << kRows) - 1), end = ln.end >> k0 & ((1u << kRows) - 1);
         const int64_t row0 = ln.row0 + k0;
         E x[G::kItems], delta[G::kItems], dy[G::kItems], z[G::kItems];
-        float h[4];
+        float h[4], slope[G::kItems], sigma[G::kItems];
 #pragma unroll
         for (int j = 0; j < G::kItems; j++) x[j] = x1[j], delta[j] = delta1[j], dy[j] = dy1[j], z[j] = z1[j];
 #pragma unroll
@@ -218,8 +219,11 @@ __global__ __launch_bounds__(Back<L>::kThreads, Back<L>::kWaves == 4 ? 2 : 1) vo
         const SelectArgs a = asked_again();
 #pragma unroll
         for (int j = 0; j < G::kItems; j++) {
-            const float d = step_of((float)delta[j] + bias), zj = (float)z[j];
-            const float o = a.z ? (float)dy[j] * (zj * gate_of<T>(zj)) : (float)dy[j];
+            const Step st = step_and_slope((float)delta[j] + bias);
+            const float d = st.d, zj = (float)z[j];
+            slope[j] = st.slope;
+            sigma[j] = a.z ? gate_of<T>(zj) : 0.0f;
+            const float o = a.z ? (float)dy[j] * (zj * sigma[j]) : (float)dy[j];
             // (channels that there are not have no part in the sums over channels)
             if (item_row + j * kItemStep < kRows)
                 s_item[item_row + j * kItemStep][item_channel] = item_channel < width ? make_float4(d, d * (float)x[j], o, 0.0f) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -320,13 +324,13 @@ __global__ __launch_bounds__(Back<L>::kThreads, Back<L>::kWaves == 4 ? 2 : 1) vo
             float o = dyj, y = got.z;
             if (b.D) y = fmaf(D, xj, y);
             if (b.z) {
-                const float s = gate_of<T>(zj);
+                const float s = sigma[j];
                 o = dyj * (zj * s);
-                static_cast<E *>(b.dz)[row * b.dz_stride + ci] = (E)(dyj * y * (s * fmaf(zj, 1.0f - s, 1.0f)));
+                (static_cast<E *>(b.dz) + row * b.dz_stride + c0)[own] = (E)(dyj * y * (s * fmaf(zj, 1.0f - s, 1.0f)));
             }
-            const float dx = b.D ? fmaf(D, o, d * eb) : d * eb, dd = fmaf(eb, xj, got.y) * step_and_slope((float)delta[j] + bias).slope;
-            static_cast<E *>(b.dx)[row * b.dx_stride + ci] = (E)dx;
-            static_cast<E *>(b.ddelta)[row * b.ddelta_stride + ci] = (E)dd;
+            const float dx = b.D ? fmaf(D, o, d * eb) : d * eb, dd = fmaf(eb, xj, got.y) * slope[j];
+            (static_cast<E *>(b.dx) + row * b.dx_stride + c0)[own] = (E)dx;
+            (static_cast<E *>(b.ddelta) + row * b.ddelta_stride + c0)[own] = (E)dd;
             dD = fmaf(o, xj, dD);
             dbias += dd;
         }

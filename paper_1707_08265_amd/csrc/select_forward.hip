@@ -139,8 +139,9 @@ void select_states(const SelectArgs &a, int wide, bool back, hipStream_t s)
 
 // Third launch.
 template <class T, int S, int L>
-__global__ __launch_bounds__(kSelectWaves *kWave) void k_select_outputs(SelectArgs a)
+__global__ __launch_bounds__(kSelectWaves *kWave) void k_select_outputs(SelectArgs args)
 {
+    const SelectArgs &a = args;
     typedef Lane<S, L> Mine;
     typedef typename T::Store E;
     __shared__ int32_t s_own[kSelectWaves][kWave];
@@ -161,6 +162,7 @@ __global__ __launch_bounds__(kSelectWaves *kWave) void k_select_outputs(SelectAr
     Column<T, kSelectBatch> x, delta, z;
     Shared<T, Mine::kWide, kSelectBatch> B, C;
     const auto fetch = [&](int k0) {
+        const SelectArgs a = asked_again();
         x.load(a.x, a.x_stride, ln.row0 + k0, ln.c, a.tokens);
         delta.load(a.delta, a.delta_stride, ln.row0 + k0, ln.c, a.tokens);
         if (a.z) z.load(a.z, a.z_stride, ln.row0 + k0, ln.c, a.tokens);
@@ -176,6 +178,7 @@ __global__ __launch_bounds__(kSelectWaves *kWave) void k_select_outputs(SelectAr
         wave_fence();
         const Column<T, kSelectBatch> x1 = x, d1 = delta, z1 = z;
         if (k0 + kSelectBatch < ln.rows) fetch(k0 + kSelectBatch);
+        const SelectArgs a = asked_again();
         if (a.kept && k0 % kSelectKeep == 0) ln.store_own(a.kept + ln.own(a, (ln.row0 + k0) / kSelectKeep), h);
         const uint32_t valid = ln.valid >> k0 & 0xff, begin = ln.begin >> k0 & 0xff, end = ln.end >> k0 & 0xff;
         E *to = static_cast<E *>(a.y) + (ln.row0 + k0) * a.y_stride + ln.c;
