@@ -59,7 +59,6 @@ struct SelectArgs {
     int32_t group_blocks;           // of channels in a group
     int32_t rows;                   // of a strip
     float *ends, *spans;            // what a strip does to a state: [strips][channels][states up to a power of two], sums of d: [strips][channels]
-    int32_t *cuts;                  // [strips]: a sequence begins (for gradients: ends) in it
     float *before, *back;           // like ends: what comes into the strip, forward and backward; NULL: few strips
     float *kept;                    // like ends, of every kSelectKeep rows: the state before that row
     float *partial, *shared;        // sums over a strip's rows and over a block's channels

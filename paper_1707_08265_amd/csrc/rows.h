@@ -96,6 +96,18 @@ __device__ __forceinline__ RowSeq sequences_of(const int64_t *rowptr, int64_t se
     const int lane = lane_id();
     own[lane] = -1;
     wave_fence();
+    const int64_t row = row0 + lane;
+    if (seqs < kWave) {                 // all pointers in one look (rows are fewer than 2^31)
+        const int32_t p = (int32_t)row_bound(lane <= seqs ? rowptr[lane] : tokens, tokens);
+        const int64_t at = p - row0;
+        if (lane <= seqs && at >= 0 && at < kWave) atomicMax(&own[at], lane);
+        wave_fence();
+        const int q0 = __popcll(__ballot(lane <= seqs && p <= row0)) - 1;
+        int q = wave_incl_max(own[lane]);
+        q = q < q0 ? q0 : q;
+        const int32_t first = __shfl(p, q < 0 ? 0 : q, kWave), end = __shfl(p, q < 0 ? 0 : q + 1 < kWave ? q + 1 : q, kWave);
+        return q >= 0 && q < seqs && row < tokens && first <= row && row < end ? RowSeq{q, first, end} : RowSeq{-1, 0, 0};
+    }
     const int64_t q0 = uniform(rows_below(rowptr, seqs + 1, row0 + 1)) - 1;       // the last pointer that is not past row0
     for (int64_t at = q0 + 1;; at += kWave) {
         const int64_t q = at + lane;
@@ -107,7 +119,6 @@ __device__ __forceinline__ RowSeq sequences_of(const int64_t *rowptr, int64_t se
     int32_t q = wave_incl_max(own[lane]);
     q = q < (int32_t)q0 ? (int32_t)q0 : q;
     RowSeq r = {-1, 0, 0};
-    const int64_t row = row0 + lane;
     if (q >= 0 && q < seqs && row < tokens) {
         const int64_t first = row_bound(rowptr[q], tokens), end = row_bound(rowptr[q + 1], tokens);
         if (first <= row && row < end) r = RowSeq{q, first, end};

@@ -51,6 +51,13 @@ template <class T> __device__ __forceinline__ float gate_of(float z)
     return inverse(1.0f + exp2_of(z * -kLog2e));
 }
 
+// What a strip does to a state.  Its sum of d says so if a sequence begins in it (sums are at least 0, or no numbers).
+constexpr float kCutSpan = -1.0f;
+__device__ __forceinline__ float apply_strip(float span, float end, float A2, float h)
+{
+    return span == kCutSpan ? end : fmaf(exp2_of(span * A2), h, end);
+}
+
 // Sum over the L lanes of a channel, L a power of two: inside a row of 16 lanes by moves (quads, then mirrors of lanes that agree).
 template <int kControl> __device__ __forceinline__ float moved(float v)
 {
@@ -173,15 +180,15 @@ template <int S, int L> struct Lane {
 #pragma unroll
         for (int i = 0; i < S; i++) h[i] = 0.0f;
         const int64_t n = kBack ? a.strips - 1 - strip : strip;
-#pragma unroll 2
+        constexpr int kAhead = S == 4 ? 8 : 2;          // (strips that are asked for at once)
+#pragma unroll kAhead
         for (int64_t k = 0; k < n; k++) {
             const int64_t at = kBack ? a.strips - 1 - k : k;
             float e[S];
             load_own(a.ends + own(a, at), e);
             const float span = a.spans[at * a.channels + c];
-            const bool cut = a.cuts[at];
 #pragma unroll
-            for (int i = 0; i < S; i++) h[i] = cut ? e[i] : fmaf(exp2_of(span * A2[i]), h[i], e[i]);
+            for (int i = 0; i < S; i++) h[i] = apply_strip(span, e[i], A2[i], h[i]);
         }
     }
 };
@@ -245,7 +252,7 @@ struct SelectLayout {
     int64_t group_blocks, blocks, rows, strips;
     int64_t back_group_blocks, back_blocks;
     int wide;
-    size_t spans, cuts, ends, before, partial, shared, copy, bytes, carry;
+    size_t spans, ends, before, partial, shared, copy, bytes, carry;
 };
 SelectLayout select_layout(const SelectArgs &a);
 void select_states(const SelectArgs &a, int wide, bool back, hipStream_t s);

@@ -20,11 +20,10 @@ __global__ __launch_bounds__(kSelectWaves *kWave) void k_select_back_ends(Select
     Mine ln;
     if (!ln.find(a, (int64_t)blockIdx.x * kSelectWaves + wave_id())) return;
     ln.mark(a, s_own[wave_id()]);
-    if (lane_id() == 0) a.cuts[ln.strip] = ln.end != 0;
     if (!(ln.valid & ~ln.begin & 1)) {
         const float none[S] = {};
         ln.store_own(a.ends + ln.own(a, ln.strip), none);
-        if (ln.active && ln.part == 0) a.spans[ln.strip * a.channels + ln.c] = 0.0f;
+        if (ln.active && ln.part == 0) a.spans[ln.strip * a.channels + ln.c] = kCutSpan;
         return;
     }
     const int to = ln.end ? __builtin_ctzll(ln.end) + 1 : ln.rows;      // rows 0 .. to - 1 are of one sequence
@@ -67,7 +66,7 @@ __global__ __launch_bounds__(kSelectWaves *kWave) void k_select_back_ends(Select
         else rows(std::true_type());
     }
     ln.store_own(a.ends + ln.own(a, ln.strip), h);
-    if (ln.active && ln.part == 0) a.spans[ln.strip * a.channels + ln.c] = span;
+    if (ln.active && ln.part == 0) a.spans[ln.strip * a.channels + ln.c] = ln.end ? kCutSpan : span;
 }
 
 // Sums of N values a lane over the lanes that are a multiple of L apart.  Lanes 32, then 16 apart share out what is left (an exchange of halves

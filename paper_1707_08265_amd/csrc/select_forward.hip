@@ -14,11 +14,10 @@ __global__ __launch_bounds__(kSelectWaves *kWave) void k_select_ends(SelectArgs 
     Mine ln;
     if (!ln.find(a, (int64_t)blockIdx.x * kSelectWaves + wave_id())) return;
     ln.mark(a, s_own[wave_id()]);
-    if (lane_id() == 0) a.cuts[ln.strip] = ln.begin != 0;       // (the same from every wave of the strip)
     if (!((ln.valid & ~ln.end) >> (ln.rows - 1) & 1)) {         // (nothing goes on past it; without a beginning no row belongs to a sequence)
         const float none[S] = {};
         ln.store_own(a.ends + ln.own(a, ln.strip), none);
-        if (ln.active && ln.part == 0) a.spans[ln.strip * a.channels + ln.c] = 0.0f;
+        if (ln.active && ln.part == 0) a.spans[ln.strip * a.channels + ln.c] = kCutSpan;
         return;
     }
     const int from = ln.begin ? 63 - __builtin_clzll(ln.begin) : 0;
@@ -58,83 +57,65 @@ __global__ __launch_bounds__(kSelectWaves *kWave) void k_select_ends(SelectArgs 
         else rows(std::true_type());
     }
     ln.store_own(a.ends + ln.own(a, ln.strip), h);
-    if (ln.active && ln.part == 0) a.spans[ln.strip * a.channels + ln.c] = span;
+    if (ln.active && ln.part == 0) a.spans[ln.strip * a.channels + ln.c] = ln.begin ? kCutSpan : span;
 }
 
-// Second launch: the state that comes into each strip.  A workgroup has kSlots neighbouring states and 1 024 / kSlots pieces of the strips: each
+// Second launch: the state that comes into each strip.  A workgroup has 64 neighbouring states and a wave for each of 16 pieces of the strips: each
 // is put together, the pieces before are applied one after the other, and each is gone through again: up to kEach strips of a piece with what
 // they do in registers, so that it is asked for once and all at once (kEach 0: any number).  256 strips of 16 384 states: 29 us without.
 constexpr int kStateThreads = 1024;
-template <int kSlots, int kEach>
+template <int kEach>
 __global__ __launch_bounds__(kStateThreads) void k_select_states(SelectArgs a, int wide, bool back)
 {
-    constexpr int kPieces = kStateThreads / kSlots;
-    __shared__ float s_end[kPieces][kSlots], s_span[kPieces][kSlots];
-    __shared__ bool s_cut[kPieces];
-    const int lane = threadIdx.x % kSlots, piece = threadIdx.x / kSlots;
-    const int64_t slots = a.channels * wide, slot = (int64_t)blockIdx.x * kSlots + lane, at = slot < slots ? slot : slots - 1;
+    constexpr int kPieces = kStateThreads / kWave;
+    __shared__ float s_end[kPieces][kWave], s_span[kPieces][kWave];
+    const int lane = lane_id(), piece = wave_id();
+    const int64_t slots = a.channels * wide, slot = (int64_t)blockIdx.x * kWave + lane, at = slot < slots ? slot : slots - 1;
     const int64_t c = divide(at, wide), n = at - c * wide;
     const float A2 = n < a.states ? a.A[c * a.states + n] * kLog2e : 0.0f;
     const int64_t each = (a.strips + kPieces - 1) / kPieces, from = piece * each, to = from + each < a.strips ? from + each : a.strips;
     float *out = back ? a.back : a.before;
     const auto strip_of = [&](int64_t k) { return back ? a.strips - 1 - k : k; };
     float end[kEach ? kEach : 1], step[kEach ? kEach : 1];
-    uint32_t cuts = 0;
-    if (kEach) {
-        static_assert(kEach <= 16 && kEach <= kSlots, "a lane for each strip of a piece");
 #pragma unroll
-        for (int k = 0; k < kEach; k++) {
-            const int64_t strip = strip_of(from + k < to ? from + k : 0);
-            end[k] = a.ends[strip * slots + at];
-            step[k] = a.spans[strip * a.channels + c];
-        }
-        const bool cut = lane < kEach && from + lane < to && a.cuts[strip_of(from + lane < to ? from + lane : 0)];
-        cuts = (uint32_t)(__ballot(cut) >> (lane_id() & ~(kSlots < kWave ? kSlots - 1 : kWave - 1)));
+    for (int k = 0; k < kEach; k++) {
+        const int64_t strip = strip_of(from + k < to ? from + k : 0);
+        end[k] = a.ends[strip * slots + at];
+        step[k] = a.spans[strip * a.channels + c];
     }
     float h = 0.0f, span = 0.0f;
-    bool any = cuts != 0;
+    bool cut = false;
     const auto every = [&](auto write) {
+        const auto one = [&](int64_t k, float e, float d) {
+            if (write.value) { if (slot < slots) out[strip_of(k) * slots + slot] = h; }
+            h = apply_strip(d, e, A2, h);
+            span += d;
+            cut = cut || d == kCutSpan;
+        };
         if (kEach) {
 #pragma unroll
-            for (int k = 0; k < kEach; k++) {
-                if (from + k >= to) break;
-                if (write.value) { if (slot < slots) out[strip_of(from + k) * slots + slot] = h; }
-                h = cuts >> k & 1 ? end[k] : fmaf(exp2_of(step[k] * A2), h, end[k]);
-                span += step[k];
-            }
+            for (int k = 0; k < kEach; k++) if (from + k < to) one(from + k, end[k], step[k]);
             return;
         }
 #pragma unroll 4
-        for (int64_t k = from; k < to; k++) {
-            const int64_t strip = strip_of(k);
-            const float e = a.ends[strip * slots + at], d = a.spans[strip * a.channels + c];
-            const bool here = a.cuts[strip];
-            if (write.value) { if (slot < slots) out[strip * slots + slot] = h; }
-            h = here ? e : fmaf(exp2_of(d * A2), h, e);
-            span += d;
-            any = any || here;
-        }
+        for (int64_t k = from; k < to; k++) one(k, a.ends[strip_of(k) * slots + at], a.spans[strip_of(k) * a.channels + c]);
     };
     every(std::false_type());
     s_end[piece][lane] = h;
-    s_span[piece][lane] = span;
-    if (lane == 0) s_cut[piece] = any;
+    s_span[piece][lane] = cut ? kCutSpan : span;
     __syncthreads();
     h = 0.0f;
 #pragma unroll 4
-    for (int p = 0; p < piece; p++) {
-        const float e = s_end[p][lane];
-        h = s_cut[p] ? e : fmaf(exp2_of(s_span[p][lane] * A2), h, e);
-    }
+    for (int p = 0; p < piece; p++) h = apply_strip(s_span[p][lane], s_end[p][lane], A2, h);
     every(std::true_type());
 }
 void select_states(const SelectArgs &a, int wide, bool back, hipStream_t s)
 {
     const int64_t slots = a.channels * wide;
     const dim3 threads(kStateThreads), few((unsigned)((slots + 63) / 64));
-    if (a.strips <= 64) hipLaunchKernelGGL((k_select_states<64, 4>), few, threads, 0, s, a, wide, back);
-    else if (a.strips <= 256) hipLaunchKernelGGL((k_select_states<64, 16>), few, threads, 0, s, a, wide, back);
-    else hipLaunchKernelGGL((k_select_states<64, 0>), few, threads, 0, s, a, wide, back);
+    if (a.strips <= 64) hipLaunchKernelGGL((k_select_states<4>), few, threads, 0, s, a, wide, back);
+    else if (a.strips <= 256) hipLaunchKernelGGL((k_select_states<16>), few, threads, 0, s, a, wide, back);
+    else hipLaunchKernelGGL((k_select_states<0>), few, threads, 0, s, a, wide, back);
 }
 
 // Third launch.
@@ -332,8 +313,7 @@ SelectLayout select_layout(const SelectArgs &a)
     l.ends = 0;
     l.before = l.ends + room(l.strips * state);
     l.spans = l.before + room(l.strips * state);
-    l.cuts = l.spans + room((size_t)l.strips * a.channels * sizeof(float));
-    l.partial = l.cuts + room((size_t)l.strips * sizeof(int32_t));
+    l.partial = l.spans + room((size_t)l.strips * a.channels * sizeof(float));
     l.copy = l.partial;             // (the one forward, the other backward)
     l.shared = l.partial + room(l.strips * (state + 2 * a.channels * sizeof(float)));
     const size_t copied = l.copy + (size_t)a.seqs * a.channels * a.states * sizeof(float),
@@ -367,7 +347,6 @@ hipError_t launch_select(int dtype, bool back, const SelectArgs &args, void *car
     a.rows = (int32_t)l.rows;
     a.ends = at(l.ends);
     a.spans = at(l.spans);
-    a.cuts = reinterpret_cast<int32_t *>(mem + l.cuts);
     a.before = a.back = l.strips > kFewStrips ? at(l.before) : nullptr;
     a.kept = static_cast<float *>(carry);
     a.partial = at(l.partial);
