@@ -612,8 +612,8 @@ int dgn_conv_step(const dgn_conv_desc *desc, int64_t num_slots, const void *x, c
  *      d = log(1 + exp(delta_t[c] + delta_bias[c]))
  *      h_t[n] = exp(d A[c][n]) h_{t-1}[n] + d x_t[c] B_t[g][n],        h_{-1} = h0 (zero without one)
  *      y_t[c] = sum_n C_t[g][n] h_t[n] + D[c] x_t[c],   times z_t[c] / (1 + exp(-z_t[c])) with z
- * States are floats.  A is at most 0 in use; exp(A times the sum of up to 64 rows' d) is formed and has to be in the range of floats.  A state
- * that is no finite number stays none in its own sequence and channel and reaches no other (but a channel's y and gradients are sums over
+ * States are floats.  A is to be at most 0: exp(A times sums of d over many rows) is formed, which with a positive A may pass the range of
+ * floats though no state does.  A state that is no finite number stays none in its own sequence and channel and reaches no other (but a channel's y and gradients are sums over
  * its states, those of B and C over the channels of a group). */
 typedef struct dgn_select_desc {
     int64_t num_tokens, num_seqs, num_channels;
@@ -645,7 +645,7 @@ typedef struct dgn_select_grads {
 } dgn_select_grads;
 
 /* Bytes of scratch for dgn_select_forward / dgn_select_backward (the larger), and of the states that a forward pass keeps for the backward
- * pass.  Either pointer may be NULL. */
+ * pass: those before every 16th row.  Either pointer may be NULL. */
 int dgn_select_workspace(const dgn_select_desc *desc, size_t *scratch_bytes, size_t *carry_bytes);
 
 /* -> y [num_tokens][num_channels], final like h0 or NULL (the state after the last token; h0 of an empty sequence; may be h0 or overlap it),

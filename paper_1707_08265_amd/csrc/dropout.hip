@@ -31,7 +31,7 @@ __device__ __forceinline__ void philox(u64 block, u64 seed, u64 offset, uint32_t
 }
 
 // kFlat: rows without gaps, taken as one.  Otherwise eight neighbours may be of two rows or more.
-template <class T, bool kResidual, bool kFlat>
+template <class T, bool kResidual, bool kFlat, bool kStream>
 __global__ __launch_bounds__(kDropThreads) void k_dropout(DropArgs a)
 {
     typedef typename T::Store S;
@@ -63,7 +63,7 @@ __global__ __launch_bounds__(kDropThreads) void k_dropout(DropArgs a)
                     out[k] = kResidual ? v + to[i].get(k) : v;
                 }
                 to[i].set(out);
-                to[i].store(y + row * a.y_stride + column + i * kPart);
+                to[i].template store<kStream>(y + row * a.y_stride + column + i * kPart);
             }
             continue;
         }
@@ -83,13 +83,19 @@ template <class T> static void go_dropout(const DropArgs &a, hipStream_t s)
     const int64_t c = a.columns, groups = (a.rows * c + kDraws * kDropThreads - 1) / (kDraws * kDropThreads);
     const dim3 grid((unsigned)(groups < (1 << 23) ? groups : 1 << 23)), threads(kDropThreads);
     const bool flat = a.rows == 1 || (a.x_stride == c && a.y_stride == c && (!a.residual || a.residual_stride == c));
+    // results of calls that are larger than the last-level cache go past it
+    const bool stream = flat && (size_t)(a.rows * c) * (a.residual ? 3 : 2) * sizeof(typename T::Store) > kStreamBytes;
+#define DGN_GO(R, F, P) hipLaunchKernelGGL((k_dropout<T, R, F, P>), grid, threads, 0, s, a)
     if (a.residual) {
-        if (flat) hipLaunchKernelGGL((k_dropout<T, true, true>), grid, threads, 0, s, a);
-        else hipLaunchKernelGGL((k_dropout<T, true, false>), grid, threads, 0, s, a);
+        if (stream) DGN_GO(true, true, true);
+        else if (flat) DGN_GO(true, true, false);
+        else DGN_GO(true, false, false);
     } else {
-        if (flat) hipLaunchKernelGGL((k_dropout<T, false, true>), grid, threads, 0, s, a);
-        else hipLaunchKernelGGL((k_dropout<T, false, false>), grid, threads, 0, s, a);
+        if (stream) DGN_GO(false, true, true);
+        else if (flat) DGN_GO(false, true, false);
+        else DGN_GO(false, false, false);
     }
+#undef DGN_GO
 }
 hipError_t launch_dropout(int dtype, const DropArgs &a, hipStream_t s)
 {
