@@ -3,7 +3,8 @@
 // The draws are those of Philox 4x32 with ten rounds (J. Salmon, M. Moraes, R. Dror, D. Shaw, "Parallel random numbers: as easy as 1, 2, 3",
 // 2011): a block of four 32-bit words is a function of a 64-bit key and a 128-bit counter, so that a thread makes the eight 16-bit draws of its
 // eight elements from their place alone, and the backward pass makes the same ones again.  16 bits a draw: with 32, twice the integer work, it
-// would be bound by that work (20 products and about 60 other instructions a block) and not by memory.
+// would be bound by that work (20 products and about 60 other instructions a block) and not by memory.  65 537 x 1 024 in bf16: with a residual 403
+// MB in 73 us (5.5 TB/s), without 268 MB in 44 (6.0; a copy has 6.2).
 #include "layer.h"
 #include "rows.h"
 
@@ -83,7 +84,7 @@ template <class T> static void go_dropout(const DropArgs &a, hipStream_t s)
     const int64_t c = a.columns, groups = (a.rows * c + kDraws * kDropThreads - 1) / (kDraws * kDropThreads);
     const dim3 grid((unsigned)(groups < (1 << 23) ? groups : 1 << 23)), threads(kDropThreads);
     const bool flat = a.rows == 1 || (a.x_stride == c && a.y_stride == c && (!a.residual || a.residual_stride == c));
-    // results of calls that are larger than the last-level cache go past it
+    // results of calls that are larger than the last-level cache go past it (65 537 x 1 024: 75.3 -> 72.7 us with a residual, 44.9 -> 44.4)
     const bool stream = flat && (size_t)(a.rows * c) * (a.residual ? 3 : 2) * sizeof(typename T::Store) > kStreamBytes;
 #define DGN_GO(R, F, P) hipLaunchKernelGGL((k_dropout<T, R, F, P>), grid, threads, 0, s, a)
     if (a.residual) {

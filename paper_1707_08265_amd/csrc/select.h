@@ -20,7 +20,10 @@ constexpr int kSelectWaves = 4;         // of a workgroup; each works by itself
 constexpr int kSelectBatch = 8;         // rows that a wave has in registers at a time
 constexpr int kSelectMostRows = 64;     // of a strip
 constexpr int kSelectKeep = 16;         // rows between two states that the forward pass keeps for the backward pass
-constexpr int64_t kFewStrips = 32;      // up to so many strips each applies the ones before it itself
+// Up to so many strips each applies the ones before it itself, half as many where a lane has 16 states (forward with that and with the launch
+// between, us: 32 strips of 512 x 2 048 x 16 27.0 and 32.5; 64 of 1 024 x 512, four states a lane, 22.3 and 23.7; 64 of 1 024 x 2 048, 16
+// states, 47.2 and 38.9; 128 of 2 048 x 512, four states, 37.6 and 34.7).
+constexpr int64_t kFewSelectStrips = 64;
 constexpr float kLog2e = 1.44269504088896340736f, kLog2eLow = 1.92596299112661746887e-8f, kLn2 = 0.69314718055994530942f;
 
 __device__ __forceinline__ float exp2_of(float v) { return __builtin_amdgcn_exp2f(v); }

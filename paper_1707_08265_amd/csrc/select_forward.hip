@@ -3,7 +3,8 @@
 
 namespace dgn {
 
-// First launch: what a strip does to the state that comes into it.
+// First launch: what a strip does to the state that comes into it.  Bound by vector instructions, seven slots of four cycles a state and row (an
+// exponential takes four of them) and 30 a row and channel: 16 384 x 1 024 x 16 in bf16 62 us, which those counts give at 2.3 GHz.
 template <class T, int S, int L>
 __global__ __launch_bounds__(kSelectWaves *kWave) void k_select_ends(SelectArgs a)
 {
@@ -118,7 +119,9 @@ void select_states(const SelectArgs &a, int wide, bool back, hipStream_t s)
     else hipLaunchKernelGGL((k_select_states<0>), few, threads, 0, s, a, wide, back);
 }
 
-// Third launch.
+// Third launch: eight slots a state and row, and 37 instructions a row and channel.  16 384 x 1 024 x 16 in bf16 95 us, 32 771 x 2 048 x 16 320 us.
+// (Four states a lane instead of 16 do what belongs to a row and channel four times over, but are four times as many waves: the rule is at
+// select_layout.)
 template <class T, int S, int L>
 __global__ __launch_bounds__(kSelectWaves *kWave) void k_select_outputs(SelectArgs args)
 {
@@ -287,9 +290,12 @@ __global__ __launch_bounds__(256) void k_select_step(SelectStepArgs s)
     }
 }
 
-// Lanes: 16 states each where that gives enough waves, else four.  Rows of a strip: as few as give kSelectStrips waves, from kSelectKeep to
-// kSelectMostRows.
-constexpr int64_t kSelectStrips = 4096, kManyWaves = 2048;
+// Lanes: 16 states each where that gives kManyWaves waves of kSelectKeep rows, else four, and from 64 states on, which four a lane spread over
+// many lanes, half as many waves (forward, us with 16 and with four: 512 x 512 x 16, 256 waves, 28.1 and 17.0; 1 024 x 512 x 16, 512 waves, 25.4 and
+// 23.8; 2 048 x 512 x 16, 1 024 waves, 31.3 and 34.7; 300 x 256 x 128, 608 waves, 27.3 and 34.7; training step of 512 x 2 048 x 16, 1 024 waves, 85 and 78).
+// Rows of a strip: as few as give kSelectStrips waves, from kSelectKeep to kSelectMostRows (8 192 waves: the states between strips of 16 384 x 1 024
+// x 16 take 29 us instead of 12, its gradients 350 instead of 328).
+constexpr int64_t kSelectStrips = 4096, kManyWaves = 1024;
 SelectLayout select_layout(const SelectArgs &a)
 {
     SelectLayout l;
@@ -300,7 +306,7 @@ SelectLayout select_layout(const SelectArgs &a)
     const int64_t back = l.wide <= 16 ? 64 : 1024 / l.wide;             // channels of a workgroup of the backward pass
     l.back_group_blocks = (share + back - 1) / back;
     l.back_blocks = l.back_group_blocks * a.groups;
-    l.S = l.wide >= 16 && blocks(16) * a.groups * ((a.tokens + kSelectKeep - 1) / kSelectKeep) >= kManyWaves ? 16 : 4;
+    l.S = l.wide >= 16 && blocks(16) * a.groups * ((a.tokens + kSelectKeep - 1) / kSelectKeep) >= (l.wide < 64 ? kManyWaves : kManyWaves / 2) ? 16 : 4;
     l.L = l.wide / l.S;
     l.group_blocks = blocks(l.S);
     l.blocks = l.group_blocks * a.groups;
@@ -347,7 +353,7 @@ hipError_t launch_select(int dtype, bool back, const SelectArgs &args, void *car
     a.rows = (int32_t)l.rows;
     a.ends = at(l.ends);
     a.spans = at(l.spans);
-    a.before = a.back = l.strips > kFewStrips ? at(l.before) : nullptr;
+    a.before = a.back = l.strips > (l.S == 4 ? kFewSelectStrips : kFewSelectStrips / 2) ? at(l.before) : nullptr;
     a.kept = static_cast<float *>(carry);
     a.partial = at(l.partial);
     a.shared = at(l.shared);
@@ -365,7 +371,9 @@ hipError_t launch_select(int dtype, bool back, const SelectArgs &args, void *car
     return hipGetLastError();
 }
 
-constexpr int64_t kManySteps = 8192;     // waves, of one block each, from which on they take several
+// Waves, of one block each, from which on they take several: 64 and 128 rows of 2 048 x 16, 8 192 and 16 384 waves, are as long as the call either
+// way; 256 rows take 16.4 us, with a block a wave 21.5.
+constexpr int64_t kManySteps = 8192;
 hipError_t launch_select_step(int dtype, const SelectStepArgs &args, hipStream_t s)
 {
     const SelectLayout l = select_layout(args.in);
