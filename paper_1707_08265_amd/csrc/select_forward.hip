@@ -63,7 +63,8 @@ __global__ __launch_bounds__(kSelectWaves *kWave) void k_select_ends(SelectArgs 
 
 // Second launch: the state that comes into each strip.  A workgroup has 64 neighbouring states and a wave for each of 16 pieces of the strips: each
 // is put together, the pieces before are applied one after the other, and each is gone through again: up to kEach strips of a piece with what
-// they do in registers, so that it is asked for once and all at once (kEach 0: any number).  256 strips of 16 384 states: 29 us without.
+// they do in registers, so that it is asked for once and all at once (kEach 0: any number).  256 strips of 16 384 states: 29 us without, 313 of
+// 6 400 15.6, and 12.9 with; with 32 a piece registers are spilled.
 constexpr int kStateThreads = 1024;
 template <int kEach>
 __global__ __launch_bounds__(kStateThreads) void k_select_states(SelectArgs a, int wide, bool back)
@@ -116,6 +117,7 @@ void select_states(const SelectArgs &a, int wide, bool back, hipStream_t s)
     const dim3 threads(kStateThreads), few((unsigned)((slots + 63) / 64));
     if (a.strips <= 64) hipLaunchKernelGGL((k_select_states<4>), few, threads, 0, s, a, wide, back);
     else if (a.strips <= 256) hipLaunchKernelGGL((k_select_states<16>), few, threads, 0, s, a, wide, back);
+    else if (a.strips <= 384) hipLaunchKernelGGL((k_select_states<24>), few, threads, 0, s, a, wide, back);
     else hipLaunchKernelGGL((k_select_states<0>), few, threads, 0, s, a, wide, back);
 }
 

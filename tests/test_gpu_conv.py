@@ -81,8 +81,8 @@ def test_states_bias_and_room_for_more_rows(dgn, states, bias, train):
 
 
 def test_many_rows_in_runs_of_every_length(dgn):
-    """Enough rows that a run has more than eight of them, up to the longest."""
-    for rows, c, dtype in [(9000, 1030, "bf16"), (9000, 530, "f32"), (60001, 1025, "f16")]:
+    """Enough rows that a run has more than eight of them, up to the longest, and results that go past the caches."""
+    for rows, c, dtype in [(9000, 1030, "bf16"), (9000, 530, "f32"), (70001, 1025, "f16")]:
         gen = torch.Generator(device="cuda").manual_seed(1)
         t = TYPES[dtype]
         rn = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731

@@ -120,3 +120,5 @@ def test_more_elements_than_one_launch_counts_in_32_bits(dgn):
         want += [p for w in lo.philox((block & 0xFFFFFFFF, block >> 32, 8, 0), (7, 0)) for p in (w & 0xFFFF, w >> 16)]
     got = b.y.view(-1)[-8000:].cpu()
     assert torch.equal(got != 0, torch.tensor(want) >= 32768)
+    b.forward(x, torch.tensor([7, 8]).cuda(), residual=x)
+    assert torch.equal(b.y.view(-1)[-8000:].cpu(), torch.where(torch.tensor(want) >= 32768, 3.0, 1.0).bfloat16())

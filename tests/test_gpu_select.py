@@ -101,6 +101,13 @@ def test_options_and_room_for_more_rows(dgn, h0, train):
         check(dgn, make([5, 0, 90], 20, 16, 1, "f32", pad=pad, h0=h0, z=k == 0, D=k == 1, bias=k == 2), 1, f"pad {pad}", train)
 
 
+@pytest.mark.parametrize("c,states,groups", [(130, 64, 1), (70, 128, 2), (41, 256, 1), (90, 32, 1), (100, 100, 2)])
+def test_channels_of_several_workgroups(dgn, c, states, groups):
+    """Sums over channels that more than one workgroup of the backward pass has, with many states."""
+    for dtype in ("bf16", "f32"):
+        check(dgn, make([33, 0, 20], c, states, groups, dtype, seed=c), groups, "several workgroups")
+
+
 def test_rows_with_gaps_and_odd_addresses(dgn):
     for dtype in TYPES:
         i, dy, dfinal = make([80, 41], 34, 12, 1, dtype)
@@ -112,9 +119,16 @@ def test_rows_with_gaps_and_odd_addresses(dgn):
         check(dgn, (i, dy, dfinal), 1, "gaps")
 
 
+# rows, channels, states: strips that a launch between them puts together, few and many of them a wave; and enough waves that a lane has 16
+# states, with one lane a channel and several
+STRIPS = [(5000, 70, 16, "bf16"), (2200, 130, 8, "f32"), (1500, 33, 64, "f16"), (20000, 24, 16, "f32"), (1000, 1090, 16, "bf16"),
+          (600, 2200, 12, "f32"), (4100, 1090, 16, "f16"), (950, 610, 32, "bf16"), (1100, 530, 20, "f32"), (700, 300, 64, "bf16"),
+          (450, 310, 64, "f32"), (700, 150, 128, "f16"), (900, 131, 100, "f32"), (700, 80, 256, "bf16"), (500, 77, 201, "f32")]
+
+
 def test_many_strips(dgn):
     """More strips than a workgroup of the launch between them has, sequences that span them, and a few channels in full."""
-    for rows, c, states, dtype in [(5000, 70, 16, "bf16"), (2200, 130, 8, "f32"), (1500, 33, 64, "f16"), (20000, 24, 16, "f32")]:
+    for rows, c, states, dtype in STRIPS:
         lens = [rows // 3, 1, 0, rows - rows // 3 - 1]
         i, dy, dfinal = make(lens, c, states, 1, dtype, seed=rows)
         b = buffers(dgn, i, 1)
