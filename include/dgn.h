@@ -613,8 +613,8 @@ int dgn_conv_step(const dgn_conv_desc *desc, int64_t num_slots, const void *x, c
  *      h_t[n] = exp(d A[c][n]) h_{t-1}[n] + d x_t[c] B_t[g][n],        h_{-1} = h0 (zero without one)
  *      y_t[c] = sum_n C_t[g][n] h_t[n] + D[c] x_t[c],   times z_t[c] / (1 + exp(-z_t[c])) with z
  * States are floats.  A is to be at most 0: exp(A times sums of d over many rows) is formed, which with a positive A may pass the range of
- * floats though no state does.  A state that is no finite number stays none in its own sequence and channel and reaches no other (but a channel's y and gradients are sums over
- * its states, those of B and C over the channels of a group). */
+ * floats though no state does.  A state that is no finite number stays none in its own sequence and channel and reaches no other (but a
+ * channel's y and gradients are sums over its states, those of B and C over the channels of a group). */
 typedef struct dgn_select_desc {
     int64_t num_tokens, num_seqs, num_channels;
     int64_t num_states;      /* 1..256 */

@@ -470,7 +470,7 @@ hipError_t launch_conv(int dtype, int activation, bool back, const ConvArgs &a, 
 template <class T, bool kSilu> static void go_step(int taps, ConvStepArgs a, hipStream_t s)
 {
     constexpr int kMost = 8 / (int)sizeof(typename T::Store);
-    const int V = a.channels % kMost == 0 ? kMost : 1;
+    const int V = a.channels % kMost == 0 ? kMost : 1;          // (a row's last lane has as many as the others)
     a.pieces = (a.channels + 256 * V - 1) / (256 * V);
     const int64_t n = a.rows * a.pieces;
     const dim3 grid((unsigned)(n < (1 << 22) ? n : 1 << 22)), threads(256);

@@ -122,7 +122,7 @@ template <int L> struct Back {
     static constexpr int kWaves = L < 4 ? L : 4, kThreads = kWaves * kWave, kWide = 4 * L;
     static constexpr int kChannels = kThreads / L;                              // of a workgroup
     static constexpr int kItems = (kSelectKeep * kChannels + kThreads - 1) / kThreads;    // rows and channels of a thread
-    static constexpr int kSumRows = kWide <= 64 ? kSelectKeep : 4;              // rows whose sums over channels are in LDS at a time
+    static constexpr int kSumRows = kWide <= 64 ? kSelectKeep : 4;              // rows whose sums over channels are in LDS at a time (up to 32 KiB)
 };
 template <class T, int L>
 __global__ __launch_bounds__(Back<L>::kThreads, Back<L>::kWaves == 4 ? 2 : 1) void k_select_gradients(SelectArgs args)
