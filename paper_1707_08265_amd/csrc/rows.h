@@ -127,8 +127,9 @@ __device__ __forceinline__ RowSeq sequences_of(const int64_t *rowptr, int64_t se
 }
 
 // States of sequences without rows, `width` elements each: out = in (or zero).  A unit is kCopySlice elements of every kCopyPhases-th of those
-// among 64 sequences; one after the other they are taken by the waves of the launch that are left for it.  (in may be out: what is read first
-// goes to registers, so that the reads do not wait for the writes.)
+// among 64 sequences; one after the other they are taken by the waves of the launch that are left for it.  (What is read goes to registers first:
+// for all that the compiler knows in may be out, and each read would wait for the write before it.  14 of 96 sequences, 32 768 floats each, by one wave for 64 sequences: 2 089 us,
+// the launch without them 355.)
 constexpr int64_t kCopySlice = 1024, kCopyPhases = 8;
 inline int64_t copy_groups(int64_t seqs, int64_t width, int waves)     // workgroups of so many waves
 {

@@ -57,7 +57,7 @@ def check(dgn, made, taps, act, dtype, what, train=True):
 
 
 LENGTHS = {"one": [1], "none": [0], "two": [2], "three": [3], "four": [4], "batch": [8], "past": [9], "run": [56, 57, 55], "ones": [1] * 130,
-           "mixed": [0, 3, 1, 0, 0, 2, 64, 0], "few": [2, 1, 3, 0, 2, 2, 1] * 9, "long": [1291], "empties": [5] + [0] * 150 + [7]}
+           "mixed": [0, 3, 1, 0, 0, 2, 64, 0], "few": [2, 1, 3, 0, 2, 2, 1] * 9, "long": [1291], "63": [2] * 63, "64": [1, 3] * 32, "65": [2] * 65, "empties": [5] + [0] * 150 + [7]}
 
 
 @pytest.mark.parametrize("lens", sorted(LENGTHS))

@@ -71,7 +71,7 @@ def check(dgn, made, groups, what, train=True):
 
 
 LENGTHS = {"one": [1], "two": [2], "none": [0], "strip": [16], "past": [17], "short": [15], "mixed": [0, 31, 1, 0, 0, 32, 33, 0, 2],
-           "ones": [1] * 70, "long": [333], "pair": [70, 0, 3, 117], "many": [5, 0, 16, 17, 1, 33] * 3, "wide": [64, 63, 65, 128]}
+           "ones": [1] * 70, "long": [333], "pair": [70, 0, 3, 117], "63": [3] * 63, "64": [2] * 64, "65": [1, 0, 4, 1, 2] * 13, "many": [5, 0, 16, 17, 1, 33] * 3, "wide": [64, 63, 65, 128]}
 
 
 @pytest.mark.parametrize("lens", sorted(LENGTHS))
