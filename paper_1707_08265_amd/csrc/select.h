@@ -64,7 +64,7 @@ __device__ __forceinline__ float apply_strip(float span, float end, float A2, fl
 // Sum over the L lanes of a channel, L a power of two: inside a row of 16 lanes by moves (quads, then mirrors of lanes that agree).
 template <int kControl> __device__ __forceinline__ float moved(float v)
 {
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), kControl, 0xf, 0xf, false));
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), kControl, 0xf, 0xf, true));
 }
 template <int L> __device__ __forceinline__ float sum_channel(float v)
 {
