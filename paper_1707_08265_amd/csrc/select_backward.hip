@@ -114,7 +114,7 @@ template <int L> __device__ __forceinline__ void sum_rows(float (&v)[4][8])
 // Third launch: a strip, kSelectKeep rows at a time, the last first: their states again from the one that is kept, with their decays, in
 // registers, then the gradients.  A workgroup has up to 64 channels; what belongs to a row and channel (step, input, gradient of the output) is
 // made once, by one thread, and handed on in LDS, and the sums over a channel's states come back the same way.
-// Bound by vector instructions: 124 a row and wave of 16 channels x 16 states, 77 % of the cycles and more with the exponentials' (16 384 x 1 024 x 16
+// Bound by vector instructions: 120 a row and wave of 16 channels x 16 states, 77 % of the cycles and more with the exponentials' (16 384 x 1 024 x 16
 // in bf16: 320 us).  The next rows are asked for while the ones after them are worked on (402 us without), and the same 16 rows with branches for
 // what begins and ends in them only where something does (497 without).
 // partial: [strips][channels][kWide], then [strips][2][channels]; shared: [parts of a group's channels][tokens][groups][2 kWide].
