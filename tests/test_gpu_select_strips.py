@@ -1,0 +1,100 @@
+"""Selective scan in strips of more than sixteen rows, as large calls have them, against its plain form in 64 bits: whole groups
+of channels, with the gradients that are sums over them."""
+import pytest
+import torch
+
+import layer_oracle as lo
+import values_oracle as vo
+
+pytestmark = pytest.mark.gpu
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+NAN = float("nan")
+ROWS, GROUPED = ("x", "delta", "z", "dy"), ("B", "C")
+GRADS = ("dx", "ddelta", "dA", "dB", "dC", "dD", "ddelta_bias", "dz", "dh0")
+
+
+@pytest.fixture(scope="module")
+def dgn():
+    assert torch.cuda.is_available(), "these tests need the GPU"
+    import paper_1707_08265_amd as d
+    return d
+
+
+def strip_rows(dgn, tokens, c, states, groups, dtype):
+    """Rows of a strip, from what a call asks for: with so many sequences, two states a strip, its sums, and a copy of h0."""
+    seqs = 2**31 - 2
+    d = dgn.dgn_select_desc(num_tokens=tokens, num_seqs=seqs, num_channels=c, num_states=states, num_groups=groups,
+                            dtype=dgn.values.DTYPES[dtype])
+    rc, need, _ = dgn.dgn_select_workspace(d)
+    assert rc == 0
+    wide = 4
+    while wide < states:
+        wide *= 2
+    room = lambda v: -(-v // 256) * 256  # noqa: E731
+    for rows in range(16, 80, 16):
+        strips = -(-tokens // rows)
+        if room(2 * room(strips * c * wide * 4) + room(strips * c * 4) + seqs * c * states * 4) == need:
+            return rows
+    raise AssertionError("strips of no known length")
+
+
+# rows, groups, channels of a group, states, type, and the rows of a strip that this is to have: one or more lanes a channel, with four
+# states each or 16; groups of one channel, of some, and of more than a wave or workgroup has
+CASES = [(613, 512, 1, 16, "bf16", 64), (601, 450, 3, 4, "f32", 64), (500, 300, 2, 8, "f16", 32), (805, 256, 1, 12, "bf16", 48),
+         (530, 512, 1, 32, "f32", 64), (530, 512, 1, 64, "f16", 64), (900, 300, 1, 128, "bf16", 64), (700, 300, 1, 256, "f32", 48),
+         (500, 150, 70, 16, "bf16", 32), (600, 256, 40, 20, "f32", 64), (565, 160, 33, 64, "bf16", 64), (610, 450, 2, 5, "bf16", 64),
+         (700, 300, 1, 3, "f16", 48)]
+
+
+@pytest.mark.parametrize("tokens,groups,share,states,dtype,rows", CASES)
+def test_long_strips(dgn, tokens, groups, share, states, dtype, rows):
+    """Sequences that begin and end in any sixteen rows of a strip, some past several strips; rows of none before and after; the
+    last strip is shorter."""
+    t, c = TYPES[dtype], groups * share
+    assert strip_rows(dgn, tokens, c, states, groups, t) == rows and tokens % 16
+    before, after, lens = 21, 83, [40, 0, 17, 1, 33, 70, 0, 15, 16]
+    lens.append(tokens - before - after - sum(lens))
+    s, ptr = len(lens), torch.tensor([before] + [before + sum(lens[:k + 1]) for k in range(len(lens))]).cuda()
+    gen = torch.Generator(device="cuda").manual_seed(tokens)
+    rn = lambda *shape: torch.randn(*shape, generator=gen, device="cuda")  # noqa: E731
+
+    def full(width):
+        v = rn(tokens, width)
+        v[:before], v[tokens - after:] = NAN, NAN
+        return v.to(t)
+    i = dict(x=full(c), delta=full(c), A=-torch.exp(rn(c, states) * 0.7), B=full(groups * states), C=full(groups * states), D=rn(c),
+             delta_bias=rn(c) * 0.5 - 2, z=full(c), h0=rn(s, c, states))
+    dy, dfinal = full(c), rn(s, c, states)
+    print(f"select strips of {rows}: {tokens} rows of {groups} x {share} x {states} {dtype}", flush=True)
+    b = dgn.SelectiveBuffers(tokens, s, c, num_states=states, num_groups=groups, dtype=t, train=True)
+    names = ("y", "dx", "ddelta", "dB", "dC", "dz")
+    for name in names:
+        getattr(b, name).fill_(7.0)
+    b.forward(**i, seq_rowptr=ptr)
+    b.backward(**i, seq_rowptr=ptr, dy=dy, dfinal=dfinal)
+    torch.cuda.synchronize()
+    inside = slice(before, tokens - after)
+    for name in ("y", "final") + GRADS:
+        got = getattr(b, name)
+        if name in names:
+            assert (got[:before] == 7.0).all() and (got[tokens - after:] == 7.0).all(), f"{name} outside the sequences"
+            got = got[inside]
+        assert got.isfinite().all(), name
+    # some groups in full
+    some = [0, groups // 2, groups - 1]
+    at = torch.tensor([g * share + k for g in some for k in range(share)]).cuda()
+    columns = torch.tensor([g * states + n for g in some for n in range(states)]).cuda()
+
+    def pick(name, v):
+        if name in ("B", "C", "dB", "dC"):
+            return v[:, columns]
+        return v[at] if name in ("A", "D", "delta_bias", "dA", "dD", "ddelta_bias") else v[:, at]
+    want = lo.select(**{k: pick(k, v) for k, v in i.items()}, rowptr=ptr, groups=3, dy=pick("dy", dy), dfinal=pick("dfinal", dfinal))
+    for name, (value, error) in want.items():
+        got = pick(name, getattr(b, name))
+        if name in names:
+            got, value, error = got[inside], value[inside], error[inside]
+        vo.within(got, value, error, name)
+    only = dgn.SelectiveBuffers(tokens, s, c, num_states=states, num_groups=groups, dtype=t)       # without states kept: the same
+    only.forward(**i, seq_rowptr=ptr)
+    assert torch.equal(only.y[inside], b.y[inside]) and torch.equal(only.final, b.final)
