@@ -54,8 +54,11 @@ template <class T> __device__ __forceinline__ float gate_of(float z)
     return inverse(1.0f + exp2_of(z * -kLog2e));
 }
 
-// What a strip does to a state.  Its sum of d says so if a sequence begins in it (sums are at least 0, or no numbers).
-constexpr float kCutSpan = -1.0f;
+// What a strip does to a state.  Its sum of d says so if a sequence begins in it (sums are at least 0, or no numbers).  A sum of finite steps that
+// passes the range of floats is its end: infinity times an A of 0, or that of a state that there is not, would be no number.  (A step that
+// is no number is in the strip's end too.)
+constexpr float kCutSpan = -1.0f, kMostSpan = 3.402823466e38f;
+__device__ __forceinline__ float kept_span(float span) { return fminf(span, kMostSpan); }
 __device__ __forceinline__ float apply_strip(float span, float end, float A2, float h)
 {
     return span == kCutSpan ? end : fmaf(exp2_of(span * A2), h, end);

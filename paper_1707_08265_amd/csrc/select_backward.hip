@@ -66,7 +66,7 @@ __global__ __launch_bounds__(kSelectWaves *kWave) void k_select_back_ends(Select
         else rows(std::true_type());
     }
     ln.store_own(a.ends + ln.own(a, ln.strip), h);
-    if (ln.active && ln.part == 0) a.spans[ln.strip * a.channels + ln.c] = ln.end ? kCutSpan : span;
+    if (ln.active && ln.part == 0) a.spans[ln.strip * a.channels + ln.c] = ln.end ? kCutSpan : kept_span(span);
 }
 
 // Sums of N values a lane over the lanes that are a multiple of L apart.  Lanes 32, then 16 apart share out what is left (an exchange of halves

@@ -58,7 +58,7 @@ __global__ __launch_bounds__(kSelectWaves *kWave) void k_select_ends(SelectArgs 
         else rows(std::true_type());
     }
     ln.store_own(a.ends + ln.own(a, ln.strip), h);
-    if (ln.active && ln.part == 0) a.spans[ln.strip * a.channels + ln.c] = ln.begin ? kCutSpan : span;
+    if (ln.active && ln.part == 0) a.spans[ln.strip * a.channels + ln.c] = ln.begin ? kCutSpan : kept_span(span);
 }
 
 // Second launch: the state that comes into each strip.  A workgroup has 64 neighbouring states and a wave for each of 16 pieces of the strips: each
@@ -104,7 +104,7 @@ __global__ __launch_bounds__(kStateThreads) void k_select_states(SelectArgs a, i
     };
     every(std::false_type());
     s_end[piece][lane] = h;
-    s_span[piece][lane] = cut ? kCutSpan : span;
+    s_span[piece][lane] = cut ? kCutSpan : kept_span(span);
     __syncthreads();
     h = 0.0f;
 #pragma unroll 4

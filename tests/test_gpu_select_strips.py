@@ -98,3 +98,35 @@ def test_long_strips(dgn, tokens, groups, share, states, dtype, rows):
     only = dgn.SelectiveBuffers(tokens, s, c, num_states=states, num_groups=groups, dtype=t)       # without states kept: the same
     only.forward(**i, seq_rowptr=ptr)
     assert torch.equal(only.y[inside], b.y[inside]) and torch.equal(only.final, b.final)
+
+
+@pytest.mark.parametrize("rows,c,states,dtype", [(100, 20, 9, "f32"), (100, 20, 16, "bf16"), (1300, 24, 5, "f32"), (2000, 40, 16, "f32"),
+                                                 (1000, 1090, 12, "bf16")])
+def test_steps_whose_sum_passes_the_range_of_floats(dgn, rows, c, states, dtype):
+    """Two steps of 3e38 in a strip: what decays is gone, a state with an A of 0 stays, and numbers of states that are no power of two
+    are as the others.  Few strips, and many that a launch between them puts together."""
+    t, rn = TYPES[dtype], lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    i = dict(x=rn(rows, c).to(t), delta=rn(rows, c).to(t), A=-torch.exp(rn(c, states) * 0.7), B=rn(rows, states).to(t),
+             C=rn(rows, states).to(t), D=rn(c), delta_bias=rn(c) * 0.5 - 2, z=rn(rows, c).to(t), h0=rn(2, c, states))
+    dy, dfinal = rn(rows, c).to(t), rn(2, c, states)
+    i["A"][3] = 0.0
+    for k in (35, 36, rows - 20, rows - 19):
+        i["delta"][k, :8], i["x"][k, :8], i["B"][k] = 3e38, 0.0, 0.0
+    ptr = torch.tensor([0, rows - 15, rows]).cuda()
+    b = dgn.SelectiveBuffers(rows, 2, c, num_states=states, dtype=t, train=True)
+    print(f"select long sums of steps: {rows} x {c} x {states} {dtype}", flush=True)
+    b.forward(**i, seq_rowptr=ptr)
+    b.backward(**i, seq_rowptr=ptr, dy=dy, dfinal=dfinal)
+    at = torch.tensor([0, 3, 7, 8, c - 1]).cuda()
+    pick = lambda n, v: v if n in ("B", "C") else v[at] if n in ("A", "D", "delta_bias", "dA", "dD", "ddelta_bias") else v[:, at]  # noqa: E731
+    want = lo.select(**{k: pick(k, v) for k, v in i.items()}, rowptr=ptr, dy=dy[:, at], dfinal=dfinal[:, at])
+    for name, (value, error) in want.items():
+        if name in ("dB", "dC"):
+            assert getattr(b, name).isfinite().all()
+            continue
+        got = pick(name, getattr(b, name))
+        if name == "dA":                    # (of an A of 0: the sum of those steps times what is there, past the range too)
+            keep = torch.tensor([0, 2, 3, 4])
+            got, value, error = got[keep.cuda()], value[keep], error[keep]
+        vo.within(got, value, error, name)
