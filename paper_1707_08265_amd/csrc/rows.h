@@ -130,11 +130,11 @@ __device__ __forceinline__ RowSeq sequences_of(const int64_t *rowptr, int64_t se
 // among 64 sequences; one after the other they are taken by the waves of the launch that are left for it.  (What is read goes to registers first:
 // for all that the compiler knows in may be out, and each read would wait for the write before it.  14 of 96 sequences, 32 768 floats each, by one wave for 64 sequences: 2 089 us,
 // the launch without them 355.)
-constexpr int64_t kCopySlice = 1024, kCopyPhases = 8;
+constexpr int64_t kCopySlice = 1024, kCopyPhases = 8, kMostCopyGroups = 1024;
 inline int64_t copy_groups(int64_t seqs, int64_t width, int waves)     // workgroups of so many waves
 {
     const int64_t units = (seqs + kWave - 1) / kWave * kCopyPhases * ((width + kCopySlice - 1) / kCopySlice), n = (units + waves - 1) / waves;
-    return n < 1024 ? n : 1024;
+    return n < kMostCopyGroups ? n : kMostCopyGroups;
 }
 template <class S> __device__ __forceinline__ void copy_empties(const int64_t *rowptr, int64_t seqs, int64_t tokens, int64_t width, const S *in, S *out,
                                                                 int64_t wave, int64_t waves)

@@ -333,7 +333,7 @@ bool select_fits(int, const SelectArgs &a)          // launches of less than 2^3
 {
     const SelectLayout l = select_layout(a);
     const int64_t most = l.blocks > l.back_blocks ? l.blocks : l.back_blocks;
-    return l.strips * most < ((int64_t)1 << 24) && a.channels * l.wide < ((int64_t)1 << 25);
+    return l.strips * most < ((int64_t)1 << 24) - kMostCopyGroups && a.channels * l.wide < ((int64_t)1 << 25);
 }
 size_t select_scratch_bytes(int, const SelectArgs &a) { return select_layout(a).bytes; }
 size_t select_carry_bytes(int, const SelectArgs &a) { return select_layout(a).carry; }

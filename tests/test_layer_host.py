@@ -219,3 +219,11 @@ def test_the_generator_gives_the_published_numbers():
     ones = 0xFFFFFFFF
     assert lo.philox((ones, ones, ones, ones), (ones, ones)) == [0x408F276D, 0x41C83B0E, 0xA20BC7C6, 0x6D5451FD]
     assert np.array_equal(lo.draws(16, 0, 0)[:8], [0xE8D5, 0x6627, 0xC58D, 0xE169, 0xAC4C, 0xBC57, 0xDBD8, 0x9B00])
+
+
+def test_the_largest_scans_fit_one_launch_with_the_empty_sequences(d):
+    """A launch of less than 2^32 threads has the strips' workgroups of 256 and up to 1 024 more, for states of sequences without rows."""
+    one = lambda groups_: select_desc(d, num_tokens=64 * groups_, num_channels=1, num_groups=1, num_states=16)  # noqa: E731
+    assert d.dgn_select_workspace(one(2**24 - 1025))[0] == 0
+    for strips in (2**24 - 1024, 2**24 - 1000, 2**24 - 1):
+        assert d.dgn_select_workspace(one(strips))[0] == d.DGN_ERR_TOO_LARGE, strips
