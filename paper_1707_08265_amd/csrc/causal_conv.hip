@@ -407,7 +407,7 @@ static ConvLayout conv_layout(int dtype, const ConvArgs &a)
 bool conv_fits(int dtype, const ConvArgs &a)        // launches of less than 2^32 threads
 {
     const ConvLayout l = conv_layout(dtype, a);
-    return l.groups * l.blocks < ((int64_t)1 << 24) - kMostCopyGroups && a.channels < ((int64_t)1 << 28);
+    return l.groups * l.blocks < ((int64_t)1 << 24) - kMostCopyGroups && a.channels <= ((int64_t)1 << 28) - kWave;
 }
 size_t conv_scratch_bytes(int dtype, const ConvArgs &a) { return conv_layout(dtype, a).bytes; }
 

@@ -227,3 +227,12 @@ def test_the_largest_scans_fit_one_launch_with_the_empty_sequences(d):
     assert d.dgn_select_workspace(one(2**24 - 1025))[0] == 0
     for strips in (2**24 - 1024, 2**24 - 1000, 2**24 - 1):
         assert d.dgn_select_workspace(one(strips))[0] == d.DGN_ERR_TOO_LARGE, strips
+
+
+def test_the_widest_convolutions_fit_one_launch(d):
+    """The sums of a tap take a workgroup of 1 024 threads for 64 channels, in launches of less than 2^32 threads."""
+    for dtype in (d.DGN_F32, d.DGN_BF16):
+        wide = lambda c: conv_desc(d, num_tokens=1, num_channels=c, dtype=dtype)  # noqa: E731
+        assert d.dgn_conv_workspace(wide(2**28 - 64))[0] == 0
+        for c in (2**28 - 63, 2**28 - 1):
+            assert d.dgn_conv_workspace(wide(c))[0] == d.DGN_ERR_TOO_LARGE, c
