@@ -619,7 +619,8 @@ typedef struct dgn_select_desc {
     int64_t num_tokens, num_seqs, num_channels;
     int64_t num_states;      /* 1..256 */
     int64_t num_groups;      /* divides num_channels */
-    int32_t dtype, reserved; /* of x, delta, B, C, z, y and their gradients */
+    int32_t dtype;           /* of x, delta, B, C, z, y and their gradients */
+    int32_t forward_only;    /* 1: no gradients will be asked for; else 0 */
     /* elements from row to row; 0 = rows without gaps */
     int64_t x_stride, delta_stride, b_stride, c_stride, z_stride, y_stride;
     int64_t dy_stride, dx_stride, ddelta_stride, db_stride, dc_stride, dz_stride;
@@ -645,7 +646,8 @@ typedef struct dgn_select_grads {
 } dgn_select_grads;
 
 /* Bytes of scratch for dgn_select_forward / dgn_select_backward (the larger), and of the states that a forward pass keeps for the backward
- * pass: those before every 16th row.  Either pointer may be NULL. */
+ * pass: those before every 16th row.  Either pointer may be NULL.  With forward_only: the scratch of dgn_select_forward, which is by far
+ * the smaller from 32 states on, and no carry; that call takes none then, and dgn_select_backward is refused (DGN_ERR_INVALID_ARG). */
 int dgn_select_workspace(const dgn_select_desc *desc, size_t *scratch_bytes, size_t *carry_bytes);
 
 /* -> y [num_tokens][num_channels], final like h0 or NULL (the state after the last token; h0 of an empty sequence; may be h0 or overlap it),

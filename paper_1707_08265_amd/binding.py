@@ -117,7 +117,7 @@ class dgn_conv_desc(ctypes.Structure):
 
 class dgn_select_desc(ctypes.Structure):
     _fields_ = [(n, c_int64) for n in ("num_tokens", "num_seqs", "num_channels", "num_states", "num_groups")] + [
-        ("dtype", c_int32), ("reserved", c_int32)] + [(n, c_int64) for n in (
+        ("dtype", c_int32), ("forward_only", c_int32)] + [(n, c_int64) for n in (
             "x_stride", "delta_stride", "b_stride", "c_stride", "z_stride", "y_stride", "dy_stride", "dx_stride",
             "ddelta_stride", "db_stride", "dc_stride", "dz_stride")]
 

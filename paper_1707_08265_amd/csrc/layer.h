@@ -71,8 +71,8 @@ struct SelectStepArgs {
     float *state_out;
 };
 bool select_fits(int dtype, const SelectArgs &a);
-size_t select_scratch_bytes(int dtype, const SelectArgs &a);
-size_t select_carry_bytes(int dtype, const SelectArgs &a);
+size_t select_scratch_bytes(const SelectArgs &a, bool forward_only);
+size_t select_carry_bytes(const SelectArgs &a);
 hipError_t launch_select(int dtype, bool back, const SelectArgs &a, void *carry, void *scratch, hipStream_t s);
 hipError_t launch_select_step(int dtype, const SelectStepArgs &a, hipStream_t s);
 

@@ -47,7 +47,8 @@ ConvArgs conv_args(const dgn_conv_desc *d)
 int check_select(const dgn_select_desc *d)
 {
     if (!d) return DGN_ERR_NULL_PTR;
-    if (!sizes_ok(d->num_tokens, d->num_seqs, d->num_channels) || !type_known(d->dtype) || d->num_states < 1 || d->num_groups < 1)
+    if (!sizes_ok(d->num_tokens, d->num_seqs, d->num_channels) || !type_known(d->dtype) || d->num_states < 1 || d->num_groups < 1 ||
+        (d->forward_only != 0 && d->forward_only != 1))
         return DGN_ERR_INVALID_ARG;
     if (d->num_tokens > kMaxCount || d->num_seqs > kMaxCount || d->num_channels > kMaxCount || d->num_states > 256) return DGN_ERR_TOO_LARGE;
     if (d->num_channels % d->num_groups || d->num_groups > kMaxCount) return DGN_ERR_INVALID_ARG;
@@ -234,8 +235,8 @@ int dgn_select_workspace(const dgn_select_desc *d, size_t *scratch_bytes, size_t
     if (rc != DGN_OK) return rc;
     const SelectArgs a = select_args(d);
     if (a.channels > 0 && !select_fits(d->dtype, a)) return DGN_ERR_TOO_LARGE;
-    if (scratch_bytes) *scratch_bytes = a.channels > 0 ? round256(select_scratch_bytes(d->dtype, a)) : 0;
-    if (carry_bytes) *carry_bytes = a.channels > 0 ? round256(select_carry_bytes(d->dtype, a)) : 0;
+    if (scratch_bytes) *scratch_bytes = a.channels > 0 ? round256(select_scratch_bytes(a, d->forward_only)) : 0;
+    if (carry_bytes) *carry_bytes = a.channels > 0 && !d->forward_only ? round256(select_carry_bytes(a)) : 0;
     return DGN_OK;
 }
 
@@ -253,7 +254,8 @@ int dgn_select_forward(const dgn_select_desc *d, const dgn_select_inputs *in, vo
     if ((d->num_tokens > 0 && !y) || (need > 0 && !scratch)) return DGN_ERR_NULL_PTR;
     if (scratch_bytes < need) return DGN_ERR_WORKSPACE_TOO_SMALL;
     const size_t e = element_size(d->dtype);
-    if (misaligned(y, e) || misaligned(final, 4) || misaligned(carry, 16) || misaligned(scratch, 16)) return DGN_ERR_INVALID_ARG;
+    if (misaligned(y, e) || misaligned(final, 4) || misaligned(carry, 16) || misaligned(scratch, 16) || (carry && d->forward_only))
+        return DGN_ERR_INVALID_ARG;
     const int64_t b = e, c = a.channels, state = c * a.states * 4;
     const Span first = dense(a.h0, a.seqs, state), last = dense(final, a.seqs, state);
     const Span out[] = {{y, a.tokens, a.y_stride * b, c * b}, dense(carry, 1, (int64_t)kept), dense(scratch, 1, (int64_t)need), last};
@@ -273,6 +275,7 @@ int dgn_select_backward(const dgn_select_desc *d, const dgn_select_inputs *in, c
     size_t need = 0, kept = 0;
     int rc = dgn_select_workspace(d, &need, &kept);
     if (rc != DGN_OK) return rc;
+    if (d->forward_only) return DGN_ERR_INVALID_ARG;
     if (!g) return DGN_ERR_NULL_PTR;
     if (d->num_channels == 0) return DGN_OK;
     if (!g->dA) return DGN_ERR_NULL_PTR;

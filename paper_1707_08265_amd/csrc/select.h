@@ -258,7 +258,7 @@ struct SelectLayout {
     int64_t group_blocks, blocks, rows, strips;
     int64_t back_group_blocks, back_blocks;
     int wide;
-    size_t spans, ends, before, partial, shared, copy, bytes, carry;
+    size_t spans, ends, before, partial, shared, copy, forward_bytes, bytes, carry;
 };
 SelectLayout select_layout(const SelectArgs &a);
 void select_states(const SelectArgs &a, int wide, bool back, hipStream_t s);

@@ -324,9 +324,9 @@ SelectLayout select_layout(const SelectArgs &a)
     l.partial = l.spans + room((size_t)l.strips * a.channels * sizeof(float));
     l.copy = l.partial;             // (the one forward, the other backward)
     l.shared = l.partial + room(l.strips * (state + 2 * a.channels * sizeof(float)));
-    const size_t copied = l.copy + (size_t)a.seqs * a.channels * a.states * sizeof(float),
-                 sums = l.shared + (size_t)l.back_group_blocks * a.tokens * a.groups * 2 * l.wide * sizeof(float);
-    l.bytes = copied > sums ? copied : sums;
+    l.forward_bytes = l.copy + (size_t)a.seqs * a.channels * a.states * sizeof(float);
+    const size_t sums = l.shared + (size_t)l.back_group_blocks * a.tokens * a.groups * 2 * l.wide * sizeof(float);
+    l.bytes = l.forward_bytes > sums ? l.forward_bytes : sums;
     return l;
 }
 bool select_fits(int, const SelectArgs &a)          // launches of less than 2^32 threads
@@ -335,8 +335,12 @@ bool select_fits(int, const SelectArgs &a)          // launches of less than 2^3
     const int64_t most = l.blocks > l.back_blocks ? l.blocks : l.back_blocks;
     return l.strips * most < ((int64_t)1 << 24) - kMostCopyGroups && a.channels * l.wide < ((int64_t)1 << 25);
 }
-size_t select_scratch_bytes(int, const SelectArgs &a) { return select_layout(a).bytes; }
-size_t select_carry_bytes(int, const SelectArgs &a) { return select_layout(a).carry; }
+size_t select_scratch_bytes(const SelectArgs &a, bool forward_only)
+{
+    const SelectLayout l = select_layout(a);
+    return forward_only ? l.forward_bytes : l.bytes;
+}
+size_t select_carry_bytes(const SelectArgs &a) { return select_layout(a).carry; }
 
 __global__ __launch_bounds__(256) void k_copy_floats(const float *from, float *to, int64_t n)
 {

@@ -101,10 +101,10 @@ class ConvStepBuffers:
                                       _queue(at, stream)), "dgn_conv_step")
 
 
-def _select_desc(tokens, seqs, channels, states, groups, dtype):
+def _select_desc(tokens, seqs, channels, states, groups, dtype, train):
     _need(dtype in DTYPES, "element type")
     return b.dgn_select_desc(num_tokens=tokens, num_seqs=seqs, num_channels=channels, num_states=states, num_groups=groups,
-                             dtype=DTYPES[dtype])
+                             dtype=DTYPES[dtype], forward_only=0 if train else 1)
 
 
 class _Selective:
@@ -137,7 +137,7 @@ class SelectiveBuffers(_Selective):
 
     def __init__(self, num_tokens, num_seqs, num_channels, num_states=16, num_groups=1, dtype=torch.bfloat16, train=False,
                  device="cuda"):
-        self._d = _select_desc(num_tokens, num_seqs, num_channels, num_states, num_groups, dtype)
+        self._d = _select_desc(num_tokens, num_seqs, num_channels, num_states, num_groups, dtype, train)
         rc, sb, cb = b.dgn_select_workspace(self._d)
         b._check(rc, "dgn_select_workspace")
         self._sizes(num_tokens, num_channels, num_states, num_groups, dtype, device)
@@ -187,7 +187,7 @@ class SelectiveStepBuffers(_Selective):
     """Output of one token of the selective scan for each of ``num_rows`` rows, on states in a pool of ``num_slots``."""
 
     def __init__(self, num_rows, num_slots, num_channels, num_states=16, num_groups=1, dtype=torch.bfloat16, device="cuda"):
-        self._d = _select_desc(num_rows, 0, num_channels, num_states, num_groups, dtype)
+        self._d = _select_desc(num_rows, 0, num_channels, num_states, num_groups, dtype, False)
         b._check(b.dgn_select_workspace(self._d)[0], "dgn_select_workspace")
         self._sizes(num_rows, num_channels, num_states, num_groups, dtype, device)
         self.num_rows, self.num_slots = num_rows, num_slots

@@ -130,3 +130,29 @@ def test_steps_whose_sum_passes_the_range_of_floats(dgn, rows, c, states, dtype)
             keep = torch.tensor([0, 2, 3, 4])
             got, value, error = got[keep.cuda()], value[keep], error[keep]
         vo.within(got, value, error, name)
+
+
+@pytest.mark.parametrize("rows,c,states,seqs", [(1, 20, 16, 3), (100, 33, 64, 5), (600, 300, 128, 9), (3000, 40, 256, 40), (2000, 1090, 5, 2)])
+def test_the_forward_pass_stays_in_the_scratch_that_it_asks_for(dgn, rows, c, states, seqs):
+    """With states that go out where they come in, whose copy is the last thing in it."""
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    rn = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    x, delta, B, C = rn(rows, c), rn(rows, c), rn(rows, states), rn(rows, states)
+    A, h0 = -torch.exp(rn(c, states)), rn(seqs, c, states)
+    ptr = torch.linspace(0, rows, seqs + 1).long().cuda()
+    outs = []
+    for only in (0, 1):
+        m = dgn.dgn_select_desc(num_tokens=rows, num_seqs=seqs, num_channels=c, num_states=states, num_groups=1, dtype=dgn.DGN_F32,
+                                forward_only=only)
+        rc, need, _ = dgn.dgn_select_workspace(m)
+        room, y, final = torch.full((need + 8192,), 7, dtype=torch.uint8, device="cuda"), torch.empty_like(x), h0.clone()
+        scratch = room[4096:4096 + need]
+        inputs = dgn.dgn_select_inputs(*(v if v is None else v.data_ptr() for v in (x, delta, A, B, C, None, None, None, ptr, final)))
+        assert rc == 0 and dgn.dgn_select_forward(m, inputs, y, final, None, scratch, need) == 0
+        assert (room[:4096] == 7).all() and (room[4096 + need:] == 7).all()
+        outs += [(y, final)]
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+    want = lo.select(x, delta, A, B, C, ptr, h0=h0) if rows * c * states < 4_000_000 else None
+    if want:
+        vo.within(outs[1][0], *want["y"], "y")
+        vo.within(outs[1][1], *want["final"], "final")

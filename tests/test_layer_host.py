@@ -236,3 +236,20 @@ def test_the_widest_convolutions_fit_one_launch(d):
         assert d.dgn_conv_workspace(wide(2**28 - 64))[0] == 0
         for c in (2**28 - 63, 2**28 - 1):
             assert d.dgn_conv_workspace(wide(c))[0] == d.DGN_ERR_TOO_LARGE, c
+
+
+def test_scans_without_gradients_ask_for_the_forward_pass_alone(d):
+    """The states of the strips, their sums of steps, and a copy of h0; no carry.  What is refused then."""
+    for states, gib in ((16, 0.07), (64, 0.28), (128, 0.56), (256, 1.1)):
+        m = dict(num_tokens=16384, num_seqs=8, num_channels=2048, num_states=states, num_groups=1)
+        rc, need, carry = d.dgn_select_workspace(select_desc(d, **m, forward_only=1))
+        both = d.dgn_select_workspace(select_desc(d, **m))
+        assert rc == 0 and carry == 0 and need < gib * 2**30 and both[0] == 0 and both[1] >= need and both[2] > 0, (states, need)
+    assert d.dgn_select_workspace(select_desc(d, forward_only=2))[0] == d.DGN_ERR_INVALID_ARG
+    m = select_desc(d, forward_only=1)
+    need, good = d.dgn_select_workspace(m)[1], apart(INPUTS + ("y", "final", "carry", "scratch"))
+    inputs = d.dgn_select_inputs(*(good[n] for n in INPUTS))
+    assert d.dgn_select_forward(m, inputs, good["y"], good["final"], good["carry"], good["scratch"], need, stream=0) == d.DGN_ERR_INVALID_ARG
+    assert d.dgn_select_forward(m, inputs, good["y"], good["final"], None, good["scratch"], need - 1, stream=0) == d.DGN_ERR_WORKSPACE_TOO_SMALL
+    grads = d.dgn_select_grads(*(64 for _ in GRADS))
+    assert d.dgn_select_backward(m, inputs, good["carry"], 64, None, grads, good["scratch"], 2**30, stream=0) == d.DGN_ERR_INVALID_ARG
