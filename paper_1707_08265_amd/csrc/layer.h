@@ -62,6 +62,7 @@ struct SelectArgs {
     float *before, *back;           // like ends: what comes into the strip, forward and backward; NULL: few strips
     float *kept;                    // like ends, of every kSelectKeep rows: the state before that row
     float *partial, *shared;        // sums over a strip's rows and over a block's channels
+    int64_t slice, slice_strips, slice_rows;    // backward: first strip, strips and rows of a launch
 };
 struct SelectStepArgs {
     SelectArgs in;                  // tokens: rows

@@ -19,6 +19,12 @@ namespace dgn {
 constexpr int kSelectWaves = 4;         // of a workgroup; each works by itself
 constexpr int kSelectBatch = 8;         // rows that a wave has in registers at a time
 constexpr int kSelectMostRows = 64;     // of a strip
+// Sums over the channels of a workgroup wait in memory for those of the others, [blocks of channels][rows][2 states], which is as much as the
+// square of the states: backward a launch takes as many strips as these many bytes have room for, but those of so many workgroups at
+// least, for what the last of a launch leave idle (backward of 16 384 x 2 048 in bf16, ms, in one launch, in ones of 256 MiB, of 4 096
+// workgroups, and as it is: 128 states 8.22, 7.87, 7.87 and 7.85, for 4.8 and 1.3 GiB of scratch; 256 states 21.1, 24.0, 22.1 and 21.7, for 17.5
+// and 2.5 GiB).
+constexpr int64_t kSharedBytes = (int64_t)256 << 20, kSharedGroups = 8192;
 constexpr int kSelectKeep = 16;         // rows between two states that the forward pass keeps for the backward pass
 // Up to so many strips each applies the ones before it itself, half as many where a lane has 16 states (forward with that and with the launch
 // between, us: 32 strips of 512 x 2 048 x 16 27.0 and 32.5; 64 of 1 024 x 512, four states a lane, 22.3 and 23.7; 64 of 1 024 x 2 048, 16
@@ -256,7 +262,7 @@ __device__ __forceinline__ SelectArgs asked_again()
 struct SelectLayout {
     int S, L;                       // forward; backward has four states a lane
     int64_t group_blocks, blocks, rows, strips;
-    int64_t back_group_blocks, back_blocks;
+    int64_t back_group_blocks, back_blocks, slice;
     int wide;
     size_t spans, ends, before, partial, shared, copy, forward_bytes, bytes, carry;
 };

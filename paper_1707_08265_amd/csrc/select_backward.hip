@@ -117,7 +117,7 @@ template <int L> __device__ __forceinline__ void sum_rows(float (&v)[4][8])
 // Bound by vector instructions: 120 a row and wave of 16 channels x 16 states, 77 % of the cycles and more with the exponentials' (16 384 x 1 024 x 16
 // in bf16: 320 us).  The next rows are asked for while the ones after them are worked on (402 us without), and the same 16 rows with branches for
 // what begins and ends in them only where something does (497 without).
-// partial: [strips][channels][kWide], then [strips][2][channels]; shared: [parts of a group's channels][tokens][groups][2 kWide].
+// partial: [strips][channels][kWide], then [strips][2][channels]; shared: [parts of a group's channels][rows of the launch][groups][2 kWide].
 template <int L> struct Back {
     static constexpr int kWaves = L < 4 ? L : 4, kThreads = kWaves * kWave, kWide = 4 * L;
     static constexpr int kChannels = kThreads / L;                              // of a workgroup
@@ -136,7 +136,7 @@ __global__ __launch_bounds__(Back<L>::kThreads, Back<L>::kWaves == 4 ? 2 : 1) vo
     __shared__ __attribute__((aligned(16))) float s_bc[2][kRows * kWide];
     __shared__ __attribute__((aligned(16))) float s_sum[G::kWaves][G::kSumRows][2 * kWide];
     const SelectArgs &a = args;
-    const int64_t strips = a.strips * a.blocks;
+    const int64_t strips = a.slice_strips * a.blocks;
     if (blockIdx.x >= strips) {
         if (a.dh0)
             copy_empties(a.rowptr, a.seqs, a.tokens, a.channels * a.states, a.dfinal, a.dh0, (blockIdx.x - strips) * G::kWaves + wave_id(),
@@ -147,6 +147,7 @@ __global__ __launch_bounds__(Back<L>::kThreads, Back<L>::kWaves == 4 ? 2 : 1) vo
     // the workgroup's channels from c0 on, of which there are `width`
     ln.strip = divide(blockIdx.x, a.blocks);
     const int64_t block = blockIdx.x - ln.strip * a.blocks;
+    ln.strip += a.slice;
     ln.group = divide(block, a.group_blocks);
     const int64_t share = a.channels / a.groups, part = block - ln.group * a.group_blocks, c0 = ln.group * share + part * G::kChannels;
     const int width = (int)(share - part * G::kChannels < G::kChannels ? share - part * G::kChannels : G::kChannels);
@@ -299,13 +300,13 @@ __global__ __launch_bounds__(Back<L>::kThreads, Back<L>::kWaves == 4 ? 2 : 1) vo
                 }
                 if (k4 % G::kSumRows == 0) {
                     __syncthreads();
-                    float *to = a.shared + part * a.tokens * a.groups * (2 * kWide) + ln.group * (2 * kWide);
+                    float *to = a.shared + ((part * a.slice_rows + row0 - a.slice * a.rows + k4) * a.groups + ln.group) * (2 * kWide);
                     for (int at = threadIdx.x; at < G::kSumRows * 2 * kWide; at += G::kThreads) {
                         const int r = at / (2 * kWide), n = at % (2 * kWide);
                         float sum = 0.0f;
 #pragma unroll
                         for (int w = 0; w < G::kWaves; w++) sum += s_sum[w][r][n];
-                        if (inside.value || k0 + k4 + r < ln.rows) to[(row0 + k4 + r) * a.groups * (2 * kWide) + n] = sum;
+                        if (inside.value || k0 + k4 + r < ln.rows) to[r * a.groups * (2 * kWide) + n] = sum;
                     }
                     if (G::kSumRows < kRows) __syncthreads();
                 }
@@ -387,18 +388,19 @@ __global__ __launch_bounds__(kSumPieces *kWave) void k_select_sums(SelectArgs a,
     else if (a.ddelta_bias) a.ddelta_bias[c - a.channels] = (float)sum;
 }
 
-// Sums over the parts of a group's channels.
+// Sums over the parts of a group's channels, of the rows of the launch before it.
 template <class T>
 __global__ __launch_bounds__(256) void k_select_shared(SelectArgs a, int wide)
 {
     typedef typename T::Store E;
-    const int64_t low = row_bound(a.rowptr[0], a.tokens), high = row_bound(a.rowptr[a.seqs], a.tokens), width = a.groups * a.states;
+    const int64_t first = a.slice * a.rows, past = first + a.slice_rows, from0 = row_bound(a.rowptr[0], a.tokens), to0 = row_bound(a.rowptr[a.seqs], a.tokens);
+    const int64_t low = from0 > first ? from0 : first, high = to0 < past ? to0 : past, width = a.groups * a.states;
     for (int64_t i = low * width + (int64_t)blockIdx.x * 256 + threadIdx.x; i < high * width; i += (int64_t)gridDim.x * 256) {
         const int64_t row = divide(i, width), at = i - row * width, group = divide(at, a.states), n = at - group * a.states;
         float b = 0.0f, c = 0.0f;
 #pragma unroll 4
         for (int64_t p = 0; p < a.group_blocks; p++) {
-            const float *from = a.shared + ((p * a.tokens + row) * a.groups + group) * (2 * wide) + n;
+            const float *from = a.shared + ((p * a.slice_rows + row - first) * a.groups + group) * (2 * wide) + n;
             b += from[0];
             c += from[wide];
         }
@@ -418,31 +420,34 @@ template <class T, int S, int L> static void go_back_ends(const SelectArgs &a, c
 }
 template <class T, int L> static void go_gradients(const SelectArgs &a, hipStream_t s)
 {
-    const int64_t groups = a.strips * a.blocks + (a.dh0 ? copy_groups(a.seqs, a.channels * a.states, Back<L>::kWaves) : 0);
+    const int64_t groups = a.slice_strips * a.blocks + (a.dh0 && a.slice == 0 ? copy_groups(a.seqs, a.channels * a.states, Back<L>::kWaves) : 0);
     if (groups > 0) hipLaunchKernelGGL((k_select_gradients<T, L>), dim3((unsigned)groups), dim3(Back<L>::kThreads), 0, s, a);
 }
-template <class T> static void go_backward(const SelectArgs &a, const SelectLayout &l, hipStream_t s)
+template <class T> static void go_backward(SelectArgs a, const SelectLayout &l, hipStream_t s)
 {
     if (a.strips > 1) {
 #define DGN_CALL(S, L) go_back_ends<T, S, L>(a, l, s)
         DGN_BY_LANES(l.S, l.L, DGN_CALL);
 #undef DGN_CALL
     }
-    switch (l.wide / 4) {
-    case 1: go_gradients<T, 1>(a, s); break;
-    case 2: go_gradients<T, 2>(a, s); break;
-    case 4: go_gradients<T, 4>(a, s); break;
-    case 8: go_gradients<T, 8>(a, s); break;
-    case 16: go_gradients<T, 16>(a, s); break;
-    case 32: go_gradients<T, 32>(a, s); break;
-    default: go_gradients<T, 64>(a, s);
+    for (a.slice = 0; a.slice == 0 || a.slice < a.strips; a.slice += l.slice) {     // (without rows: what belongs to sequences alone)
+        a.slice_strips = a.strips - a.slice < l.slice ? a.strips - a.slice : l.slice;
+        a.slice_rows = a.tokens - a.slice * a.rows < l.slice * a.rows ? a.tokens - a.slice * a.rows : l.slice * a.rows;
+        switch (l.wide / 4) {
+        case 1: go_gradients<T, 1>(a, s); break;
+        case 2: go_gradients<T, 2>(a, s); break;
+        case 4: go_gradients<T, 4>(a, s); break;
+        case 8: go_gradients<T, 8>(a, s); break;
+        case 16: go_gradients<T, 16>(a, s); break;
+        case 32: go_gradients<T, 32>(a, s); break;
+        default: go_gradients<T, 64>(a, s);
+        }
+        if (a.strips == 0) break;
+        const int64_t n = (a.slice_rows * a.groups * a.states + 255) / 256;
+        hipLaunchKernelGGL((k_select_shared<T>), dim3((unsigned)(n < 8192 ? n : 8192)), dim3(256), 0, s, a, l.wide);
     }
     const int64_t sums = (a.channels * (l.wide + 2) + kWave - 1) / kWave;
     hipLaunchKernelGGL(k_select_sums, dim3((unsigned)sums), dim3(kSumPieces * kWave), 0, s, a, l.wide);
-    if (a.strips > 0) {
-        const int64_t n = (a.tokens * a.groups * a.states + 255) / 256;
-        hipLaunchKernelGGL((k_select_shared<T>), dim3((unsigned)(n < 8192 ? n : 8192)), dim3(256), 0, s, a, l.wide);
-    }
 }
 void select_backward(int dtype, const SelectArgs &a, const SelectLayout &l, hipStream_t s)
 {

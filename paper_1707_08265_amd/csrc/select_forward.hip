@@ -324,8 +324,12 @@ SelectLayout select_layout(const SelectArgs &a)
     l.partial = l.spans + room((size_t)l.strips * a.channels * sizeof(float));
     l.copy = l.partial;             // (the one forward, the other backward)
     l.shared = l.partial + room(l.strips * (state + 2 * a.channels * sizeof(float)));
+    const int64_t strip_sums = l.back_blocks * l.rows * 2 * l.wide * (int64_t)sizeof(float);
+    const int64_t fitting = kSharedBytes / strip_sums, least = (kSharedGroups + l.back_blocks - 1) / l.back_blocks;
+    l.slice = fitting > least ? fitting : least;
+    const int64_t slice_rows = l.slice * l.rows < a.tokens ? l.slice * l.rows : a.tokens;
     l.forward_bytes = l.copy + (size_t)a.seqs * a.channels * a.states * sizeof(float);
-    const size_t sums = l.shared + (size_t)l.back_group_blocks * a.tokens * a.groups * 2 * l.wide * sizeof(float);
+    const size_t sums = l.shared + (size_t)(l.back_blocks * slice_rows) * 2 * l.wide * sizeof(float);
     l.bytes = l.forward_bytes > sums ? l.forward_bytes : sums;
     return l;
 }

@@ -46,8 +46,7 @@ CASES = [(613, 512, 1, 16, "bf16", 64), (601, 450, 3, 4, "f32", 64), (500, 300, 
          (700, 300, 1, 3, "f16", 48)]
 
 
-@pytest.mark.parametrize("tokens,groups,share,states,dtype,rows", CASES)
-def test_long_strips(dgn, tokens, groups, share, states, dtype, rows):
+def check_long_strips(dgn, tokens, groups, share, states, dtype, rows):
     """Sequences that begin and end in any sixteen rows of a strip, some past several strips; rows of none before and after; the
     last strip is shorter."""
     t, c = TYPES[dtype], groups * share
@@ -98,6 +97,26 @@ def test_long_strips(dgn, tokens, groups, share, states, dtype, rows):
     only = dgn.SelectiveBuffers(tokens, s, c, num_states=states, num_groups=groups, dtype=t)       # without states kept: the same
     only.forward(**i, seq_rowptr=ptr)
     assert torch.equal(only.y[inside], b.y[inside]) and torch.equal(only.final, b.final)
+
+
+@pytest.mark.parametrize("tokens,groups,share,states,dtype,rows", CASES)
+def test_long_strips(dgn, tokens, groups, share, states, dtype, rows):
+    check_long_strips(dgn, tokens, groups, share, states, dtype, rows)
+
+
+@pytest.mark.parametrize("tokens,groups,share,states,dtype", [(1111, 256, 8, 256, "bf16"), (2201, 256, 5, 200, "f32"), (4100, 300, 1, 32, "f16"),
+                                                              (1610, 300, 17, 128, "f32")])
+def test_sums_over_channels_in_several_launches(dgn, tokens, groups, share, states, dtype):
+    """Gradients whose sums over the channels of a group do not fit the scratch at once, with sequences that go on from launch to launch."""
+    c, wide = groups * share, 32 if states <= 32 else 128 if states <= 128 else 256
+    need = lambda only: dgn.dgn_select_workspace(dgn.dgn_select_desc(  # noqa: E731
+        num_tokens=tokens, num_seqs=0, num_channels=c, num_states=states, num_groups=groups, dtype=dgn.values.DTYPES[TYPES[dtype]],
+        forward_only=only))[1]
+    blocks = groups * -(-share // (1024 // wide))
+    strips = -(-tokens // 64)
+    sums = need(0) - need(1) - strips * (c * wide + 2 * c) * 4
+    assert sums < blocks * tokens * 2 * wide * 4 * 0.95
+    check_long_strips(dgn, tokens, groups, share, states, dtype, 64)
 
 
 @pytest.mark.parametrize("rows,c,states,dtype", [(100, 20, 9, "f32"), (100, 20, 16, "bf16"), (1300, 24, 5, "f32"), (2000, 40, 16, "f32"),
@@ -156,3 +175,24 @@ def test_the_forward_pass_stays_in_the_scratch_that_it_asks_for(dgn, rows, c, st
     if want:
         vo.within(outs[1][0], *want["y"], "y")
         vo.within(outs[1][1], *want["final"], "final")
+
+
+@pytest.mark.parametrize("rows,c,states,groups", [(1, 20, 16, 1), (100, 33, 64, 3), (600, 300, 128, 1), (3000, 40, 256, 2), (700, 1090, 5, 1),
+                                                  (2201, 1280, 200, 256)])
+def test_the_gradients_stay_in_the_scratch_that_they_ask_for(dgn, rows, c, states, groups):
+    """And what it holds before does not matter."""
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    rn = lambda *s: torch.randn(*s, generator=gen, device="cuda").bfloat16()  # noqa: E731
+    i = dict(x=rn(rows, c), delta=rn(rows, c), A=-torch.exp(rn(c, states).float()), B=rn(rows, groups * states), C=rn(rows, groups * states))
+    ptr, dy = torch.tensor([0, rows // 3, rows // 3, rows]).cuda(), rn(rows, c)
+    b, seen = dgn.SelectiveBuffers(rows, 3, c, num_states=states, num_groups=groups, train=True), []
+    for fill in (0, 255):                           # (of bytes of 255, floats are no numbers)
+        room = torch.full((b._scratch_bytes + 8192,), fill, dtype=torch.uint8, device="cuda")
+        b._scratch = room[4096:4096 + b._scratch_bytes]
+        b.forward(**i, seq_rowptr=ptr)
+        b._scratch.fill_(fill)
+        b.backward(**i, seq_rowptr=ptr, dy=dy)
+        assert (room[:4096] == fill).all() and (room[-4096:] == fill).all()
+        seen.append([getattr(b, n).clone() for n in GRADS if n != "dz"])
+    for name, one, two in zip([n for n in GRADS if n != "dz"], *seen):
+        assert torch.equal(one, two) and one.isfinite().all(), name

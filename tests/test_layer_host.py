@@ -253,3 +253,11 @@ def test_scans_without_gradients_ask_for_the_forward_pass_alone(d):
     assert d.dgn_select_forward(m, inputs, good["y"], good["final"], None, good["scratch"], need - 1, stream=0) == d.DGN_ERR_WORKSPACE_TOO_SMALL
     grads = d.dgn_select_grads(*(64 for _ in GRADS))
     assert d.dgn_select_backward(m, inputs, good["carry"], 64, None, grads, good["scratch"], 2**30, stream=0) == d.DGN_ERR_INVALID_ARG
+
+
+def test_the_scratch_of_scans_grows_with_the_states_and_not_with_their_square(d):
+    """The gradients' sums over channels go through a buffer of 256 MiB, or of some thousand workgroups' rows; the rest is three states a strip."""
+    for states, gib in ((64, 0.7), (128, 1.4), (256, 2.6)):
+        m = select_desc(d, num_tokens=16384, num_seqs=8, num_channels=2048, num_states=states, num_groups=1)
+        rc, need, _ = d.dgn_select_workspace(m)
+        assert rc == 0 and need < gib * 2**30, (states, need / 2**30)
