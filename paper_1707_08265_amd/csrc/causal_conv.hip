@@ -6,8 +6,9 @@
 //
 // A wave takes a run of rows of 64 V channels and goes down (backward: up) it, eight rows in registers with the K-1 before them.  Which
 // rows sequences begin and end with is the same for the wave; eight rows in the middle of a sequence ask for nothing, rows whose window reaches
-// into a state look there.  Bound by memory: training step of 65 301 x 1 024 in f16, 268 MB forward in 54 us (4.9 TB/s; a copy has 6.2) and 403
-// MB backward in 93 (4.3; its products, two transcendentals and 16 others an element, are half of that time).
+// into a state look there.  Bound by memory: training step of 65 301 x 1 024 in f16, 268 MB forward in 54 us (4.9 TB/s; a copy has 6.2), vector units
+// 46 % busy, and 403 MB backward in 93 to 96 (4.2 to 4.3), 58 % busy with under three waves a SIMD, which wait for memory 39 % of their time.
+// (Times of calls on the same tensors, half of whose inputs the last-level cache has kept; a training step on others is 3 us longer.)
 #include "layer.h"
 #include "rows.h"
 

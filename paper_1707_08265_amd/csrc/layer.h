@@ -1,4 +1,5 @@
-// Internal declarations of the operators of a selective recurrent layer (causal_conv.hip, selective_scan.hip, dropout.hip).
+// Internal declarations of the operators of a selective recurrent layer (causal_conv.hip, select_forward.hip, select_backward.hip,
+// dropout.hip).
 #pragma once
 
 #include "values.h"

@@ -7,8 +7,8 @@
 // comes into it is h -> exp(A sum d) h + E (E its end from a state of zero), or h -> E if a sequence begins in it.  Three launches: the
 // strips' (sum d, E), which only the rows from the last beginning on have a part in, and none where the strip's last row ends a sequence; the
 // states between strips; the strips again, now with the state that comes into each (two launches for few strips, one for a single one).
-// It is bound by vector instructions: a state and row takes an exponential, which costs four others, and three or four more in each of the
-// two passes over the rows.
+// It is bound by vector instructions: a state and row takes an exponential, which costs two others (3.5 ns an instruction and SIMD; a
+// multiply-add 1.5), and three or four more in each of the two passes over the rows.
 #pragma once
 
 #include "layer.h"

@@ -8,7 +8,7 @@
 
 namespace dgn {
 
-// First launch: what a strip does to what comes back into it, from its last row to its first; only the rows up to the first end have a part
+// First launch (110 instructions a row and wave of 64 channels x 16 states, 73 % of its cycles): what a strip does to what comes back into it, from its last row to its first; only the rows up to the first end have a part
 // in it, and none where the strip's first row begins a sequence.
 template <class T, int S, int L>
 __global__ __launch_bounds__(kSelectWaves *kWave) void k_select_back_ends(SelectArgs a)
@@ -114,8 +114,8 @@ template <int L> __device__ __forceinline__ void sum_rows(float (&v)[4][8])
 // Third launch: a strip, kSelectKeep rows at a time, the last first: their states again from the one that is kept, with their decays, in
 // registers, then the gradients.  A workgroup has up to 64 channels; what belongs to a row and channel (step, input, gradient of the output) is
 // made once, by one thread, and handed on in LDS, and the sums over a channel's states come back the same way.
-// Bound by vector instructions: 120 a row and wave of 16 channels x 16 states, 77 % of the cycles and more with the exponentials' (16 384 x 1 024 x 16
-// in bf16: 320 us).  The next rows are asked for while the ones after them are worked on (402 us without), and the same 16 rows with branches for
+// Bound by vector instructions: 119 a row and wave of 16 channels x 16 states, 77 % of the cycles with the exponentials' second slots, waves for
+// 24 % of their time behind memory, LDS or the others of their workgroup (16 384 x 1 024 x 16 in bf16: 312 us).  The next rows are asked for while the ones after them are worked on (402 us without), and the same 16 rows with branches for
 // what begins and ends in them only where something does (497 without).
 // partial: [strips][channels][kWide], then [strips][2][channels]; shared: [parts of a group's channels][rows of the launch][groups][2 kWide].
 template <int L> struct Back {

@@ -3,8 +3,9 @@
 
 namespace dgn {
 
-// First launch: what a strip does to the state that comes into it.  Bound by vector instructions, seven slots of four cycles a state and row (an
-// exponential takes four of them) and 30 a row and channel: 16 384 x 1 024 x 16 in bf16 62 us, which those counts give at 2.3 GHz.
+// First launch: what a strip does to the state that comes into it.  Bound by vector instructions, 99 a row and wave of 64
+// channels x 16 states, 64 of them the states' (an exponential takes two slots of four cycles): 16 384 x 1 024 x 16 in bf16 63 us, 80 % of its
+// cycles; its waves, four a SIMD, are for 14 % of their time behind memory or LDS.
 template <class T, int S, int L>
 __global__ __launch_bounds__(kSelectWaves *kWave) void k_select_ends(SelectArgs a)
 {
@@ -121,7 +122,8 @@ void select_states(const SelectArgs &a, int wide, bool back, hipStream_t s)
     else hipLaunchKernelGGL((k_select_states<0>), few, threads, 0, s, a, wide, back);
 }
 
-// Third launch: eight slots a state and row, and 37 instructions a row and channel.  16 384 x 1 024 x 16 in bf16 95 us, 32 771 x 2 048 x 16 320 us.
+// Third launch: 143 instructions a row and wave of 64 channels x 16 states, 80 of them the states'.  16 384 x 1 024 x 16 in bf16 95 us, 76 % of the
+// cycles in vector instructions, waves for 20 % of their time behind memory or LDS; 32 771 x 2 048 x 16 316 to 338 us.
 // (Four states a lane instead of 16 do what belongs to a row and channel four times over, but are four times as many waves: the rule is at
 // select_layout.)
 template <class T, int S, int L>
@@ -228,8 +230,9 @@ template <int K> __device__ __forceinline__ float of_lane(float v, int k)
 }
 // One token for each row: four states a lane, kBlocks of a row's channel blocks a wave.  Bound by memory: all that is read is asked for before
 // anything is made of it, and what belongs to a channel (step, input, outer gate) is made by one lane: lane k of the first kBlocks for block k.
-// kFours: a multiple of four states.  States of calls larger than the last-level cache go past it: 1 024 rows of 2 048 x 16, 278 MB, in 53 us
-// (5.2 TB/s; else 64; with what belongs to a channel made by all its lanes 82, and with a block a wave 88).
+// kFours: a multiple of four states.  States of calls larger than the last-level cache go past it: 1 024 rows of 2 048 x 16, 278 MB, 65 us on a
+// pool that is not in that cache (4.3 TB/s; a copy has 6.2; A, 131 KB, is read from L2 for each row, another 134 MB).  On one pool again and
+// again, half of it in that cache, 46 to 54 (else 64; with what belongs to a channel made by all its lanes 82, and with a block a wave 88).
 template <class T, int L, int kBlocks, bool kFours, bool kStream>
 __global__ __launch_bounds__(256) void k_select_step(SelectStepArgs s)
 {
